@@ -44,7 +44,9 @@
 extern "C" {
 #endif
 
-typedef enum { CASK_F32 = 0, CASK_BF16 = 1 } cask_dtype;
+/* CASK_E4M3 (8-bit floating point: 4 exponent bits, 3 of significand, largest value 448, no infinity) is a type
+ * of cached rows alone: cask_pages.type. */
+typedef enum { CASK_F32 = 0, CASK_BF16 = 1, CASK_E4M3 = 2 } cask_dtype;
 
 /* return codes */
 enum {
@@ -306,6 +308,82 @@ int cask_attend_ws(const cask_params* params, int32_t n_units, const void* Q, co
                    int32_t count_pitch, void* out, void* ws, size_t ws_bytes, void* hip_stream);
 /* HOST: bytes cask_attend_ws makes use of; 0 where one workgroup per unit is the better choice. */
 size_t cask_attend_workspace_bytes(const cask_params* params, int32_t n_units, int32_t stride_rows);
+
+/* ---- Paged caches: rows written (quantised), read back, attended to -------------------------------------
+ *
+ * Units end an event with different numbers of rows, so every unit has a page table of its own into pools of
+ * pages that all units share.  Row r of unit u lies at pool row
+ *     table[u * table_pitch + r / page_rows] * page_pitch + r % page_rows,
+ * and without a table (NULL) at u * page_pitch + r: a buffer [n_units, page_pitch, d] such as
+ * cask_compress_step's K_out, V_out.  An entry outside [0, n_pages) says that no page is there (not written
+ * yet, or given back behind a sliding window): its rows are not written, read as zeros, and no query sees
+ * them.  Neither does any call touch rows outside the unit's capacity, table_pitch * page_rows (page_rows
+ * without a table) rows.  Pages may be shared by units that only read them; a call that writes one row of a
+ * pool for two units leaves either's there.
+ *
+ * CASK_E4M3 pools hold a row x as 8-bit values q with a float of its own, in the 2 d + 8 bytes that a row of K
+ * and V then takes (4 d in bfloat16):
+ *     a = max |x_c| over the finite channels, at least 448 * 2^-126,
+ *     scale = a / 448,  q_c = 448 x_c / a to the next e4m3 value (ties to even),  x_c ~ q_c * scale;
+ * an infinite channel becomes +-448 (the row's largest finite magnitude), a NaN stays one. */
+typedef struct {
+  int32_t type;        /* CASK_E4M3, or params->dtype */
+  int32_t n_units;
+  int32_t n_pages;     /* pages of the pools (without a table >= n_units) */
+  int32_t page_rows;   /* a power of two, 16 to 2^20; without a table any number >= 1 (CASK_E4M3: of 16s) */
+  int64_t page_pitch;  /* pool rows from the start of a page to that of the next, >= page_rows; a row has d
+                          elements in K and V, one in the scales */
+  int32_t table_pitch; /* entries per unit, table_pitch * page_rows <= 2^30 */
+  const int32_t* table; /* DEVICE [n_units, table_pitch] or NULL */
+  void* K;             /* DEVICE, 16-byte aligned: pool of keys, row 0 of page 0 */
+  void* V;             /* DEVICE, 16-byte aligned */
+  float* K_scale;      /* DEVICE, CASK_E4M3: a scale per row; else not used */
+  float* V_scale;
+} cask_pages;
+
+/* The rows of one call: unit u brings (asks for, queries from) n[u] rows; the t-th of them is row start[u] + t of
+ * the unit and row first[u] + t * pitch of the call's arrays.  Arrays [tokens, heads, ...] with the tokens of all
+ * sequences back to back: first = tokens before the sequence * heads + head, pitch = heads; arrays [n_units, max_n,
+ * ...]: first NULL, pitch 1. */
+typedef struct {
+  int32_t max_n;        /* HOST: n[u] is taken as at most this; sizes the launch */
+  int64_t pitch;        /* >= 1 */
+  int64_t total;        /* rows of the call's arrays: rows outside [0, total) are neither read nor written */
+  const int32_t* n;     /* DEVICE [n_units]; a negative one counts as 0 */
+  const int32_t* start; /* DEVICE [n_units] or NULL: 0 */
+  const int64_t* first; /* DEVICE [n_units] or NULL: u * max_n */
+} cask_rows;
+
+/* Writes K, V [total, d] (DEVICE, params->dtype, 16-byte aligned) into the pages.  Rows of the pools that no row of
+ * the call goes to are left as they are. */
+int cask_cache_write(const cask_params* params, const cask_pages* pages, const cask_rows* rows, const void* K,
+                     const void* V, void* hip_stream);
+
+/* Reads rows back into K, V [total, d] (DEVICE, params->dtype, 16-byte aligned): the values a row stands for, rounded
+ * once (copies where the pool has the same type); zeros where no page is.  Other rows of K, V are left as they are. */
+int cask_cache_read(const cask_params* params, const cask_pages* pages, const cask_rows* rows, void* K, void* V,
+                    void* hip_stream);
+
+/* Attention of the tokens of `rows` over their unit's pages, their own rows among them (cask_cache_write first).
+ * Q, out [total, G, d] (DEVICE, params->dtype, 16-byte aligned): row first[u] + t * pitch holds the G heads of the
+ * token at row i = start[u] + t.  It sees the rows j of its unit with
+ *     0 <= j < start[u] + n[u];  j <= i where params->causal;  where window > 0, j > i - window or j < sinks;
+ * and computes out = sum_j p_j v_j, p = softmax_j(scale * <q, k_j> + ln(count_j)), zeros if it sees none; what rows
+ * that it does not see hold, NaN included, has no effect on it (a value that it sees and that is not finite makes
+ * its channel of the result not finite).  fp32 accumulation, rounded once.
+ *   count [n_units, count_pitch] DEVICE or NULL, as in cask_attend: the tokens a row stands for (< 1 and rows at or
+ *         behind count_pitch: 1)
+ *   window, sinks  >= 0; window 0: every row; sinks are used with a window only
+ *   max_rows  HOST: about the largest start + n of the units, 0 = the capacity; only a choice of how the work is
+ *         dealt out goes by it (the same value gives the same bits)
+ *   ws    DEVICE, 16-byte aligned: where few queries see many rows, several workgroups share them and leave partial
+ *         results there; NULL or fewer bytes than cask_attend_paged_workspace_bytes(): one workgroup does it all. */
+int cask_attend_paged(const cask_params* params, const cask_pages* pages, const cask_rows* rows, const void* Q,
+                      const int32_t* count, int32_t count_pitch, int32_t window, int32_t sinks, int32_t max_rows,
+                      void* out, void* ws, size_t ws_bytes, void* hip_stream);
+/* HOST: bytes cask_attend_paged makes use of for such a call (device pointers are not looked at); 0: none. */
+size_t cask_attend_paged_workspace_bytes(const cask_params* params, const cask_pages* pages, const cask_rows* rows,
+                                         int32_t window, int32_t sinks, int32_t max_rows);
 
 /* Measurement aid (not part of the method): per-stage timing of cask_compress with HIP
  * events recorded on the caller's stream between its kernels.  Stage order: 0 score sweep A

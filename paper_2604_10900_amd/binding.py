@@ -19,7 +19,7 @@ import torch
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libcask.so")
 
-F32, BF16 = 0, 1
+F32, BF16, E4M3 = 0, 1, 2   # (E4M3: of cached rows alone)
 OK, EINVAL, ENOMEM, EDEVICE = 0, -1, -2, -3
 ST_ACTIVE, ST_IDENTITY, ST_PREFIX_BUDGET_EXHAUSTED, ST_MERGE_INACTIVE = 0, 1, 2, 4
 PATH_NO_FUSED_TAIL, PATH_NO_FUSED_SCORE, PATH_DEDUP_VECTOR, PATH_ATTEND_VECTOR, PATH_NO_FUSED_SWEEPS = 1, 2, 4, 8, 16   # (PATH_ATTEND_VECTOR: obsolete, no effect)
@@ -32,7 +32,8 @@ PATH_WIDE_ROWS = 128
 EXPORTS = ["cask_plan", "cask_workspace_bytes", "cask_score", "cask_prefix_evict",
            "cask_partition", "cask_consolidate", "cask_compress", "cask_compress_static", "cask_compress_step",
            "cask_mass_diagnostics", "cask_group_diagnostics", "cask_attend", "cask_attend_ws",
-           "cask_attend_workspace_bytes", "cask_strerror",
+           "cask_attend_workspace_bytes", "cask_cache_write", "cask_cache_read", "cask_attend_paged",
+           "cask_attend_paged_workspace_bytes", "cask_strerror",
            "cask_timing_enable", "cask_timing_enable_stages", "cask_timing_read",
            "cask_probe_issue", "cask_probe_copy", "cask_probe_read"]
 STAGES = ["score_rows", "score_cols", "select", "index_roles", "similarity", "gather", "emit"]
@@ -64,6 +65,17 @@ class _Batch(C.Structure):
 class _Plan(C.Structure):
     _fields_ = [("r_eff", C.c_int32), ("p_keep", C.c_int32), ("slots", C.c_int32),
                 ("core", C.c_int32), ("seeds", C.c_int32), ("status", C.c_int32)]
+
+
+class _Pages(C.Structure):
+    _fields_ = [("type", C.c_int32), ("n_units", C.c_int32), ("n_pages", C.c_int32), ("page_rows", C.c_int32),
+                ("page_pitch", C.c_int64), ("table_pitch", C.c_int32), ("table", C.c_void_p), ("K", C.c_void_p),
+                ("V", C.c_void_p), ("K_scale", C.c_void_p), ("V_scale", C.c_void_p)]
+
+
+class _Rows(C.Structure):
+    _fields_ = [("max_n", C.c_int32), ("pitch", C.c_int64), ("total", C.c_int64), ("n", C.c_void_p),
+                ("start", C.c_void_p), ("first", C.c_void_p)]
 
 
 class _ImageSlot:
@@ -202,6 +214,10 @@ def load():
             "cask_attend": (C.c_int, [vp, i32, vp, vp, vp, i32, vp, vp, i32, vp, vp]),
             "cask_attend_ws": (C.c_int, [vp, i32, vp, vp, vp, i32, vp, vp, i32, vp, vp, sz, vp]),
             "cask_attend_workspace_bytes": (sz, [vp, i32, i32]),
+            "cask_cache_write": (C.c_int, [vp] * 6),
+            "cask_cache_read": (C.c_int, [vp] * 6),
+            "cask_attend_paged": (C.c_int, [vp, vp, vp, vp, vp, i32, i32, i32, i32, vp, vp, sz, vp]),
+            "cask_attend_paged_workspace_bytes": (sz, [vp, vp, vp, i32, i32, i32]),
             "cask_strerror": (C.c_char_p, [C.c_int]),
             "cask_timing_enable": (C.c_int, [C.c_int]),
             "cask_timing_enable_stages": (C.c_int, [C.c_int, C.c_int]),
@@ -425,6 +441,136 @@ def attend(p: Params, Q: torch.Tensor, K_c: torch.Tensor, V_c: torch.Tensor, len
                             _dptr(ws), n_ws, _stream())
     if rc:
         raise CaskError("cask_attend", rc)
+    return out
+
+
+_ROW_DTYPES = {torch.float32: F32, torch.bfloat16: BF16, torch.float8_e4m3fn: E4M3}
+
+
+def _on(device: torch.device, *tensors) -> None:
+    """All of them on `device`, which is the current one: the stream a call goes to is the current device's."""
+    for t in tensors:
+        assert t is None or t.device == device, (t.device, device)
+    current = _raw_device() if _raw_device is not None else torch.cuda.current_device()
+    assert device.type == "cuda" and device.index == current, f"tensors on {device}, current device {current}"
+
+
+class Pages:
+    """A paged cache (cask_pages): the pools and who owns which page.  Keep it as long as the cache; what the tensors
+    hold may change at any time.
+
+    K, V      [n_pages, page_rows, d] float32 or bfloat16 (as p.dtype) or float8_e4m3fn; rows one behind the other,
+              pages at any common stride of whole rows (both pools may be views of one [n_pages, 2, page_rows, d])
+    K_scale, V_scale  e4m3: [n_pages, page_rows] float32, pages at the pools' stride in rows
+    table     [n_units, pages per unit] int32, -1 where no page is; None: page u is unit u's (the [n_units, stride, d]
+              buffers of an event)
+    """
+
+    def __init__(self, p: Params, K: torch.Tensor, V: torch.Tensor, K_scale: Optional[torch.Tensor] = None,
+                 V_scale: Optional[torch.Tensor] = None, table: Optional[torch.Tensor] = None):
+        assert K.dim() == 3 and K.shape == V.shape and K.stride() == V.stride() and K.dtype == V.dtype
+        n_pages, page_rows, d = K.shape
+        assert d == p.head_dim and K.stride(2) == 1 and (page_rows <= 1 or K.stride(1) == d) and K.stride(0) % d == 0
+        pitch = K.stride(0) // d if n_pages > 1 else page_rows
+        kind = _ROW_DTYPES[K.dtype]
+        if kind == E4M3:
+            for s in (K_scale, V_scale):
+                assert s is not None and s.dtype == torch.float32 and s.shape == (n_pages, page_rows) and s.stride(1) == 1
+                assert n_pages <= 1 or s.stride(0) == pitch, "pages of the scales at the stride of the pools, in rows"
+        else:
+            assert K_scale is None and V_scale is None
+        if table is not None:
+            assert table.dtype == torch.int32 and table.dim() == 2 and table.is_contiguous()
+        for t in (K, V, K_scale, V_scale, table):
+            assert t is None or (t.is_cuda and t.device == K.device), "device-resident tensors expected"
+        self.params, self.K, self.V, self.K_scale, self.V_scale, self.table = p, K, V, K_scale, V_scale, table
+        self.device = K.device
+        self.n_units = n_pages if table is None else table.shape[0]
+        ptr = [None if t is None else t.data_ptr() for t in (table, K, V, K_scale, V_scale)]
+        self._c = _Pages(kind, self.n_units, n_pages, page_rows, pitch, 0 if table is None else table.shape[1], *ptr)
+
+    @classmethod
+    def empty(cls, p: Params, n_units: int, rows: int, dtype: torch.dtype = torch.float8_e4m3fn, page_rows: int = 64,
+              device="cuda") -> "Pages":
+        """A cache of its own pages for n_units units of up to `rows` rows, nothing written."""
+        per = -(-rows // page_rows)
+        shape = (n_units * per, page_rows)
+        K = torch.zeros(*shape, p.head_dim, dtype=dtype, device=device)
+        scales = [torch.zeros(shape, dtype=torch.float32, device=device) for _ in range(2)] if dtype == torch.float8_e4m3fn else [None, None]
+        table = torch.arange(n_units * per, dtype=torch.int32, device=device).view(n_units, per)
+        return cls(p, K, torch.zeros_like(K), *scales, table=table)
+
+
+class Rows:
+    """The rows of a call (cask_rows): unit u has n[u] <= max_n of them, the t-th is row start[u] + t of the unit and
+    row first[u] + t * pitch of the call's arrays.
+
+    n, start  [n_units] int32 on the device (start None: 0)
+    first     [n_units] int64 on the device, None: u * max_n (arrays [n_units, max_n, ...])
+    """
+
+    def __init__(self, n: torch.Tensor, max_n: int, start: Optional[torch.Tensor] = None,
+                 first: Optional[torch.Tensor] = None, pitch: int = 1):
+        assert n.dtype == torch.int32 and n.dim() == 1 and n.is_cuda and n.is_contiguous()
+        for t, dt in ((start, torch.int32), (first, torch.int64)):
+            assert t is None or (t.dtype == dt and t.shape == n.shape and t.device == n.device and t.is_contiguous())
+        self.n, self.start, self.first, self.max_n, self.pitch = n, start, first, int(max_n), int(pitch)
+        self._ptr = [None if t is None else t.data_ptr() for t in (n, start, first)]
+
+    def c(self, total: int) -> _Rows:
+        return _Rows(self.max_n, self.pitch, total, *self._ptr)
+
+
+def _paged_arrays(pages: Pages, rows: Rows, per_row: int, *arrays) -> int:
+    """Rows of the call's arrays, `per_row` elements each, after the checks that all paged calls share."""
+    want = torch.float32 if pages.params.dtype == F32 else torch.bfloat16
+    for t in arrays:
+        assert t.dtype == want and t.is_contiguous() and t.shape == arrays[0].shape, (t.dtype, want, t.shape)
+        assert t.shape[-1] == pages.params.head_dim and t.numel() % per_row == 0
+    assert rows.n.numel() == pages.n_units, (rows.n.numel(), pages.n_units)
+    _on(pages.device, rows.n, *arrays)
+    return arrays[0].numel() // per_row
+
+
+def cache_write(pages: Pages, rows: Rows, K: torch.Tensor, V: torch.Tensor) -> None:
+    """Rows of K, V [..., d] into the pages, quantised if they are e4m3 (cask_cache_write)."""
+    p = pages.params
+    cp, cr = p.c(), rows.c(_paged_arrays(pages, rows, p.head_dim, K, V))
+    rc = load().cask_cache_write(C.byref(cp), C.byref(pages._c), C.byref(cr), K.data_ptr(), V.data_ptr(), _stream())
+    if rc:
+        raise CaskError("cask_cache_write", rc)
+
+
+def cache_read(pages: Pages, rows: Rows, K: torch.Tensor, V: torch.Tensor):
+    """Rows of the pages back into K, V [..., d], as the values they stand for (cask_cache_read)."""
+    p = pages.params
+    cp, cr = p.c(), rows.c(_paged_arrays(pages, rows, p.head_dim, K, V))
+    rc = load().cask_cache_read(C.byref(cp), C.byref(pages._c), C.byref(cr), K.data_ptr(), V.data_ptr(), _stream())
+    if rc:
+        raise CaskError("cask_cache_read", rc)
+    return K, V
+
+
+def attend_paged(pages: Pages, rows: Rows, Q: torch.Tensor, count: Optional[torch.Tensor] = None, window: int = 0,
+                 sinks: int = 0, max_rows: int = 0, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Attention of the tokens of `rows` over their units' pages (cask_attend_paged): Q [..., G, d], count [n_units,
+    pitch] int32 or None.  Rows of `out` that no token of the call has are left as they are (zeros if it is made here)."""
+    p = pages.params
+    if out is None:
+        out = torch.zeros_like(Q)
+    assert Q.shape[-2] == p.q_per_kv
+    cr = rows.c(_paged_arrays(pages, rows, p.q_per_kv * p.head_dim, Q, out))
+    if count is not None:
+        assert count.dtype == torch.int32 and count.dim() == 2 and count.shape[0] == pages.n_units and count.is_contiguous()
+        assert count.device == pages.device
+    cp, lib = p.c(), load()
+    n_ws = lib.cask_attend_paged_workspace_bytes(C.byref(cp), C.byref(pages._c), C.byref(cr), window, sinks, max_rows)
+    ws = torch.empty(n_ws, dtype=torch.uint8, device=pages.device) if n_ws else None
+    rc = lib.cask_attend_paged(C.byref(cp), C.byref(pages._c), C.byref(cr), Q.data_ptr(),
+                               None if count is None else count.data_ptr(), 0 if count is None else count.shape[1],
+                               window, sinks, max_rows, out.data_ptr(), None if ws is None else ws.data_ptr(), n_ws, _stream())
+    if rc:
+        raise CaskError("cask_attend_paged", rc)
     return out
 
 

@@ -9,7 +9,7 @@ ROOT = os.path.dirname(_HERE)
 CSRC = os.path.join(_HERE, "csrc")
 LIB_PATH = os.path.join(_HERE, "libcask.so")
 SOURCES = ["cask_api.hip", "cask_score.hip", "cask_select.hip", "cask_merge.hip", "cask_tail.hip", "cask_attend.hip", "cask_seed.hip",
-           "cask_probe.hip"]
+           "cask_probe.hip", "cask_paged.hip", "cask_paged_attend.hip"]
 
 
 def hipcc() -> str:

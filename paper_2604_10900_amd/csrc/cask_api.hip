@@ -266,6 +266,69 @@ struct StageRecorder {
   }
 };
 
+// The host side of a paged cache and of a call's rows: checked, and as the kernels take them.
+static bool misaligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) != 0; }
+
+// `pointers`: the device pointers are checked as well (not where only sizes are asked for).
+static int resolve_pages(const KParams& kp, const cask_pages* p, PagesView* pg, bool pointers) {
+  if (!p || p->n_units < 0) return CASK_EINVAL;
+  if (p->type != CASK_E4M3 && p->type != kp.dtype) return CASK_EINVAL;
+  if (p->n_pages < 0 || p->page_rows < 1 || p->page_pitch < p->page_rows || p->page_pitch > (1ll << 40)) return CASK_EINVAL;
+  pg->n_units = p->n_units;
+  pg->n_pages = p->n_pages;
+  pg->table_pitch = p->table_pitch;
+  pg->pitch = p->page_pitch;
+  pg->table = p->table;
+  if (p->table) {
+    if (p->page_rows < 16 || p->page_rows > (1 << 20) || (p->page_rows & (p->page_rows - 1)) || p->table_pitch < 1) return CASK_EINVAL;
+    if ((int64_t)p->table_pitch * p->page_rows > (1 << 30)) return CASK_EINVAL;
+    pg->shift = __builtin_ctz((unsigned)p->page_rows);
+    pg->mask = p->page_rows - 1;
+    pg->cap = p->table_pitch * p->page_rows;
+  } else {
+    if (p->page_rows > (1 << 30) || p->n_pages < p->n_units) return CASK_EINVAL;
+    if (p->type == CASK_E4M3 && p->page_rows % 16) return CASK_EINVAL;
+    pg->shift = 31;
+    pg->mask = 0x7fffffff;
+    pg->cap = p->page_rows;
+  }
+  pg->K = static_cast<unsigned char*>(p->K);
+  pg->V = static_cast<unsigned char*>(p->V);
+  pg->K_scale = p->K_scale;
+  pg->V_scale = p->V_scale;
+  if (!pointers || p->n_units == 0) return CASK_OK;
+  if (p->n_pages > 0) {
+    if (!p->K || !p->V || misaligned16(p->K) || misaligned16(p->V)) return CASK_EINVAL;
+    if (p->type == CASK_E4M3 && (!p->K_scale || !p->V_scale)) return CASK_EINVAL;
+  }
+  return CASK_OK;
+}
+
+static int resolve_rows(const KParams& kp, const PagesView& pg, const cask_rows* r, RowsView* rw, bool pointers) {
+  if (!r || r->max_n < 0 || r->pitch < 1 || r->total < 0 || r->total > (1ll << 40)) return CASK_EINVAL;
+  if ((int64_t)r->max_n * kp.G > (1 << 30) || (int64_t)r->max_n * pg.n_units > 0x7fffffffll) return CASK_EINVAL;
+  if (pointers && pg.n_units > 0 && r->max_n > 0 && !r->n) return CASK_EINVAL;
+  rw->max_n = r->max_n;
+  rw->pitch = r->pitch;
+  rw->total = r->total;
+  rw->n = r->n;
+  rw->start = r->start;
+  rw->first = r->first;
+  return CASK_OK;
+}
+
+static int paged_max_rows(const PagesView& pg, int max_rows) { return max_rows > 0 && max_rows < pg.cap ? max_rows : pg.cap; }
+
+// Everything about a paged call but its arrays; *none: there is nothing to do.
+static int resolve_paged(const cask_params* params, const cask_pages* pages, const cask_rows* rows, KParams* kp,
+                         PagesView* pg, RowsView* rw, bool pointers, bool* none) {
+  int rc = resolve_params(params, kp, false);
+  if (!rc) rc = resolve_pages(*kp, pages, pg, pointers);
+  if (!rc) rc = resolve_rows(*kp, *pg, rows, rw, pointers);
+  *none = !rc && (pg->n_units == 0 || rw->max_n == 0 || rw->total == 0);
+  return rc;
+}
+
 }  // namespace cask
 
 using namespace cask;
@@ -458,6 +521,68 @@ size_t cask_attend_workspace_bytes(const cask_params* params, int32_t n_units, i
   KParams kp;
   if (resolve_params(params, &kp, false) != CASK_OK || n_units < 1 || stride_rows < 1) return 0;
   return attend_part_bytes(kp, n_units, attend_splits(kp, n_units, stride_rows));
+}
+
+int cask_cache_write(const cask_params* params, const cask_pages* pages, const cask_rows* rows, const void* K,
+                     const void* V, void* hip_stream) {
+  KParams kp;
+  PagesView pg;
+  RowsView rw;
+  bool none;
+  const int rc = resolve_paged(params, pages, rows, &kp, &pg, &rw, true, &none);
+  if (rc) return rc;
+  if (none) return CASK_OK;
+  if (!K || !V || misaligned16(K) || misaligned16(V)) return CASK_EINVAL;
+  return dev_rc(launch_cache_write(kp, pg, rw, pages->type == CASK_E4M3, K, V, static_cast<hipStream_t>(hip_stream)));
+}
+
+int cask_cache_read(const cask_params* params, const cask_pages* pages, const cask_rows* rows, void* K, void* V,
+                    void* hip_stream) {
+  KParams kp;
+  PagesView pg;
+  RowsView rw;
+  bool none;
+  const int rc = resolve_paged(params, pages, rows, &kp, &pg, &rw, true, &none);
+  if (rc) return rc;
+  if (none) return CASK_OK;
+  if (!K || !V || misaligned16(K) || misaligned16(V)) return CASK_EINVAL;
+  return dev_rc(launch_cache_read(kp, pg, rw, pages->type == CASK_E4M3, K, V, static_cast<hipStream_t>(hip_stream)));
+}
+
+int cask_attend_paged(const cask_params* params, const cask_pages* pages, const cask_rows* rows, const void* Q,
+                      const int32_t* count, int32_t count_pitch, int32_t window, int32_t sinks, int32_t max_rows,
+                      void* out, void* ws, size_t ws_bytes, void* hip_stream) {
+  KParams kp;
+  PagedAttend pa;
+  bool none;
+  const int rc = resolve_paged(params, pages, rows, &kp, &pa.pg, &pa.rw, true, &none);
+  if (rc) return rc;
+  if (window < 0 || sinks < 0 || max_rows < 0 || (count && count_pitch < 1)) return CASK_EINVAL;
+  if (none) return CASK_OK;
+  if (!Q || !out || misaligned16(Q) || misaligned16(out) || misaligned16(ws)) return CASK_EINVAL;
+  const bool e4m3 = pages->type == CASK_E4M3;
+  pa.Q = Q;
+  pa.out = out;
+  pa.count = count;
+  pa.count_pitch = count_pitch;
+  pa.window = window;
+  pa.sinks = sinks;
+  pa.part = static_cast<float*>(ws);
+  pa.splits = ws ? paged_splits(kp, pa.pg.n_units, pa.rw.max_n, e4m3, window, sinks, paged_max_rows(pa.pg, max_rows)) : 1;
+  if (paged_part_bytes(kp, pa.pg.n_units, pa.rw.max_n, pa.splits) > ws_bytes) pa.splits = 1;
+  return dev_rc(launch_attend_paged(kp, pa, e4m3, static_cast<hipStream_t>(hip_stream)));
+}
+
+size_t cask_attend_paged_workspace_bytes(const cask_params* params, const cask_pages* pages, const cask_rows* rows,
+                                         int32_t window, int32_t sinks, int32_t max_rows) {
+  KParams kp;
+  PagesView pg;
+  RowsView rw;
+  bool none;
+  if (resolve_paged(params, pages, rows, &kp, &pg, &rw, false, &none) != CASK_OK || none) return 0;
+  if (window < 0 || sinks < 0 || max_rows < 0) return 0;
+  return paged_part_bytes(kp, pg.n_units, rw.max_n,
+                          paged_splits(kp, pg.n_units, rw.max_n, pages->type == CASK_E4M3, window, sinks, paged_max_rows(pg, max_rows)));
 }
 
 int cask_compress(const cask_params* params, const cask_batch* batch, void* K_out, void* V_out,

@@ -358,4 +358,75 @@ hipError_t launch_group_fold(const KParams& kp, const Batch& b, const uint8_t* r
                              int32_t* merged_ord, int32_t* seg_row, int32_t* assign_out, int32_t* status, const CopyJob& copy,
                              hipStream_t st);
 
+// ---------------------------------------------------------------- paged caches
+
+// A paged cache as the kernels see it (cask_pages, checked): row r of unit u is at pool row
+// entry * pitch + (r & mask), entry = table[u * table_pitch + (r >> shift)]; without a table the unit is
+// its own entry (shift 31, mask all ones).
+struct PagesView {
+  int n_units, n_pages, table_pitch, shift, mask;
+  int cap;        // rows a unit has room for
+  int64_t pitch;  // pool rows from page to page
+  const int32_t* table;
+  unsigned char* K;
+  unsigned char* V;
+  float* K_scale;
+  float* V_scale;
+};
+
+// The rows of a call (cask_rows, checked).
+struct RowsView {
+  int max_n;
+  int64_t pitch, total;
+  const int32_t* n;
+  const int32_t* start;
+  const int64_t* first;
+};
+
+#if defined(__HIPCC__)
+__device__ inline int rows_of_unit(const RowsView& rw, int u) {
+  const int n = rw.n[u];
+  return n < 0 ? 0 : (n < rw.max_n ? n : rw.max_n);
+}
+__device__ inline int64_t first_of_unit(const RowsView& rw, int u) {
+  return rw.first ? rw.first[u] : (int64_t)u * rw.max_n;
+}
+// Place of row t of the call in its arrays, -1 if that is outside them (no product or sum here wraps: 0 <= t < 2^30,
+// and a row this far on is compared before it is multiplied).
+__device__ inline int64_t array_row(const RowsView& rw, int64_t first, int t) {
+  if (first < 0 || first >= rw.total) return -1;
+  const int64_t left = rw.total - 1 - first;
+  if (rw.pitch > left && t > 0) return -1;
+  const int64_t at = (int64_t)t * rw.pitch;  // pitch <= total < 2^40 here
+  return at <= left ? first + at : -1;
+}
+// Pool row of row r of unit u, 0 <= r < cap; -1 where no page is.
+__device__ inline int64_t pool_row(const PagesView& pg, int u, int r) {
+  const int e = pg.table ? pg.table[(int64_t)u * pg.table_pitch + (r >> pg.shift)] : u;
+  return (unsigned)e < (unsigned)pg.n_pages ? e * pg.pitch + (r & pg.mask) : -1;
+}
+#endif
+
+hipError_t launch_cache_write(const KParams& kp, const PagesView& pg, const RowsView& rw, bool e4m3, const void* K,
+                              const void* V, hipStream_t st);
+hipError_t launch_cache_read(const KParams& kp, const PagesView& pg, const RowsView& rw, bool e4m3, void* K, void* V,
+                             hipStream_t st);
+
+// Attention over a paged cache: what its kernels are given.
+struct PagedAttend {
+  PagesView pg;
+  RowsView rw;
+  const void* Q;
+  void* out;
+  const int32_t* count;
+  int count_pitch;
+  int window, sinks;  // window 0: none
+  int splits;         // workgroups that share the rows of a block of queries
+  float* part;        // their partial results
+};
+// Splits of such a call (max_rows: about the largest number of rows a unit holds) and the bytes of their results.
+int paged_splits(const KParams& kp, int n_units, int max_n, bool e4m3, int window, int sinks, int max_rows);
+size_t paged_part_bytes(const KParams& kp, int n_units, int max_n, int splits);
+hipError_t launch_attend_paged(const KParams& kp, const PagedAttend& pa, bool e4m3, hipStream_t st);
+
 }  // namespace cask
