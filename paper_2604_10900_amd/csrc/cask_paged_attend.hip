@@ -526,6 +526,434 @@ __global__ __launch_bounds__(256) void paged_combine_kernel(int G, PagedAttend p
   Elem<T>::store(static_cast<T*>(pa.out) + (row * G + m % G) * D + ch, joined(num, den));
 }
 
+// ---------------------------------------------------------------- chunks of many query rows
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+
+struct ChunkParams {
+  int G, causal;
+  float scale_log2;
+};
+
+template <int D>
+struct ChunkGeom {
+  static constexpr int kWaveQ = 32, kWaves = 8, kBlockQ = kWaveQ * kWaves;  // query rows of a wave, of a workgroup
+  static constexpr int kStage = 64;                     // cache rows of a ring slot, eight from each wave
+  static constexpr int kRowB = D * 2;                   // bytes of a row in LDS: bf16
+  static constexpr int kSlotK = kStage * kRowB;         // keys of a slot; its values lie behind them
+  static constexpr int kSlot = 2 * kSlotK;
+  static constexpr int kDepth = 4;
+  static constexpr int kAux = kStage * 3;               // floats of a slot: bias, key scale, value scale of a row
+  static constexpr int kLds = kDepth * (kSlot + kAux * 4 + 32);
+  // Rows lie in LDS in groups of four, the group's 16-byte pieces one behind the other, each of them for its four
+  // rows; every other group has its neighbouring pieces swapped.  Eight rows' reads of one piece (keys), and four
+  // rows' reads of two neighbouring pieces (values), then meet 128 bytes that lie together.
+  __device__ static int place(int row, int piece) {
+    return (row >> 2) * (4 * kRowB) + ((piece ^ ((row >> 2) & 1)) * 4 + (row & 3)) * 16;
+  }
+};
+
+// A wave holds 32 query rows in registers, a workgroup of eight waves 256; the cache's rows come through a ring of
+// 64-row slots in LDS.  Per 32 rows of the cache, on 32x32 matrix tiles:
+//   logits   S[key][query]     = K . Q^T      (lane: query = lane % 32; keys (i & 3) + 8 (i >> 2) + 4 (lane / 32))
+//   values   O[channel][query] += V^T . P     (P as the lane has it: the product's key order is that of S; V^T by
+//                                              transposing reads of four keys)
+// Softmax: weights relative to a reference that follows the largest logit so far only when that has grown by more
+// than 2^8 (results are quotients of two sums with the same reference; nothing overflows below 2^127): then, and
+// only then, the sums are rescaled.  The three parts work on different rows in one turn of the loop -- the logits of
+// the next 32, the weights of these, the values of those before -- so that matrix and vector pipes are both busy.
+// bf16 weights are rounded once (2^-9 of a weight at the most): two terms as for single tokens would cost as many
+// matrix instructions again where these are the bound.
+template <bool E4M3, int D>
+__global__ __launch_bounds__(512, 2) void paged_chunk_kernel(ChunkParams kp, PagedAttend pa, int q_blocks) {
+  using A = ChunkGeom<D>;
+  constexpr int NK = D / 16, CB = D / 32;
+  extern __shared__ __align__(16) unsigned char ring[];
+  float* aux_all = reinterpret_cast<float*>(ring + A::kDepth * A::kSlot);
+  int* flag_all = reinterpret_cast<int*>(aux_all + A::kDepth * A::kAux);
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int c32 = lane & 31, h = lane >> 5;
+  int u, part_of;
+  if (!map_block(pa.pg.n_units, q_blocks * pa.splits, u, part_of)) return;
+  const int qb = q_blocks - 1 - part_of / pa.splits, sp = part_of % pa.splits;  // (blocks that see most rows first)
+  const int G = kp.G;
+  const UnitRows ur(pa.pg, pa.rw, u);
+  const int m0 = qb * A::kBlockQ, m_all = ur.n * G;
+  if (m0 >= m_all) return;
+  const int m1 = min(m_all, m0 + A::kBlockQ);
+  const TileRange range = tiles_of<A::kStage>(ur.start + m0 / G, ur.start + (m1 - 1) / G, ur.end, kp.causal, pa.window, pa.sinks);
+  // this workgroup's share of the stages
+  const int per = (range.n_tiles + pa.splits - 1) / pa.splits;
+  const int s_begin = min(range.n_tiles, sp * per), n_stages = min(range.n_tiles, s_begin + per) - s_begin;
+
+  const float c = kp.scale_log2;
+  const int32_t* cu = pa.count ? pa.count + (size_t)u * pa.count_pitch : nullptr;
+  // the wave's queries
+  const int w0 = m0 + wv * A::kWaveQ;
+  const int w_lo = ur.start + min(w0, m_all - 1) / G, w_hi = ur.start + min(w0 + A::kWaveQ - 1, m_all - 1) / G;
+  bf16x8 q[NK];
+  int qi;
+  {
+    const int m = w0 + c32, t = m / G;
+    const int64_t at = m < m1 ? array_row(pa.rw, ur.first, t) : -1;
+    qi = ur.start + t;
+    const uint16_t* qp = static_cast<const uint16_t*>(pa.Q) + ((at < 0 ? 0 : at) * G + (at < 0 ? 0 : m % G)) * D + h * 8;
+#pragma unroll
+    for (int k = 0; k < NK; ++k) {
+      const u32x4 v = *reinterpret_cast<const u32x4*>(qp + k * 16);
+      q[k] = __builtin_bit_cast(bf16x8, at < 0 ? u32x4{0u, 0u, 0u, 0u} : v);
+    }
+  }
+
+  // ---- the ring: wave wv brings rows [8 wv, 8 wv + 8) of a stage, all of one page
+  auto stage_row = [&](int s) { return range.tile(s_begin + s) * A::kStage; };
+  auto my_row = [&](int s) { return stage_row(s) + wv * 8; };
+  auto pool_of = [&](int s) -> int64_t {
+    const int r = my_row(s);
+    return s < n_stages && r < ur.end ? pool_row(pa.pg, u, r) : -1;
+  };
+  constexpr int EL = E4M3 ? 1 : 2, ROWB = D * EL;
+  auto rsrc_of = [&](const unsigned char* pool, int64_t row, int r) {
+    const int bytes = __builtin_amdgcn_readfirstlane((row >= 0 ? min(8, ur.end - r) : 0) * ROWB);
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char*>(pool) + (row >= 0 ? row : 0) * ROWB, 0, bytes, 0x00020000);
+  };
+  // bf16: straight to LDS, a KB an instruction; e4m3: sixteen bytes a lane, into LDS as bf16 a stage later
+  constexpr int kLoads = 8 * D / 512;               // bf16: instructions of eight rows
+  constexpr int kLanesPerRow = D / 16;              // e4m3: lanes that share a row, 16 bytes each
+  constexpr int kE4Lanes = 8 * kLanesPerRow;        // lanes that bring some
+  u32x4 ek, ev;
+  float a_bias = 0.f, a_ks = 0.f, a_vs = 0.f;       // of row lane % 8 of the wave's eight
+  auto issue = [&](int s) {
+    const int64_t row = pool_of(s);
+    const int r = my_row(s);
+    const __amdgpu_buffer_rsrc_t rk = rsrc_of(pa.pg.K, row, r), rv = rsrc_of(pa.pg.V, row, r);
+    unsigned char* slot = ring + (s % A::kDepth) * A::kSlot + wv * 8 * A::kRowB;
+    if constexpr (!E4M3) {
+#pragma unroll
+      for (int j = 0; j < kLoads; ++j) {
+        // lane -> group of four rows, piece, row of the group, as they lie in LDS
+        constexpr int kPieces = D / 8, kGroupLanes = 4 * kPieces;   // (64 channels: two groups an instruction)
+        const int grp = j * (64 / kGroupLanes) + lane / kGroupLanes;
+        const int piece = (lane % kGroupLanes) / 4 ^ (grp & 1);
+        const int off = (grp * 4 + lane % 4) * ROWB + piece * 16;
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rk, (__attribute__((address_space(3))) void*)(slot + j * 1024), 16, off, 0, 0, 0);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rv, (__attribute__((address_space(3))) void*)(slot + A::kSlotK + j * 1024), 16, off, 0, 0, 0);
+      }
+    } else {
+      ek = __builtin_amdgcn_raw_buffer_load_b128(rk, lane * 16, 0, 0);   // (64 channels: the upper lanes read zeros)
+      ev = __builtin_amdgcn_raw_buffer_load_b128(rv, lane * 16, 0, 0);
+    }
+    a_bias = kNegInf;
+    const int mine = r + (lane & 7);
+    if (row >= 0 && mine < ur.end) {
+      a_bias = 0.f;
+      if (cu && mine < pa.count_pitch) a_bias = (float)cu[mine];
+      if constexpr (E4M3) {
+        a_ks = pa.pg.K_scale[row + (lane & 7)];
+        a_vs = pa.pg.V_scale[row + (lane & 7)];
+      }
+    }
+  };
+  auto commit = [&](int s) {  // what came through registers, into the slot
+    float* aux = aux_all + (s % A::kDepth) * A::kAux + wv * 8;
+    const float bias = a_bias > 1.f ? __log2f(a_bias) : (a_bias == kNegInf ? kNegInf : 0.f);
+    if (lane < 8) {
+      aux[lane] = bias;
+      if constexpr (E4M3) {
+        aux[A::kStage + lane] = a_ks * c;
+        aux[2 * A::kStage + lane] = a_vs;
+      }
+    }
+    const int f = __any(bias != 0.f);
+    if (lane == 0) flag_all[(s % A::kDepth) * 8 + wv] = f;
+    if constexpr (E4M3) {
+      unsigned char* slot = ring + (s % A::kDepth) * A::kSlot;
+      const int r = wv * 8 + lane / kLanesPerRow, piece = (lane % kLanesPerRow) * 2;
+      if (lane < kE4Lanes) {
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          u32x4 k, v;
+#pragma unroll
+          for (int w = 0; w < 4; ++w) {
+            k[w] = e4m3_to_bf16(ek[2 * e + w / 2], w & 1);
+            v[w] = e4m3_to_bf16(ev[2 * e + w / 2], w & 1);
+          }
+          *reinterpret_cast<u32x4*>(slot + A::place(r, piece + e)) = k;
+          *reinterpret_cast<u32x4*>(slot + A::kSlotK + A::place(r, piece + e)) = v;
+        }
+      }
+    }
+  };
+  // every wave's share of every stage issued so far has landed, and the slot used before last is free
+  auto meet = [&]() {
+    __builtin_amdgcn_s_waitcnt(0x0070);  // vmcnt(0) lgkmcnt(0)
+    __builtin_amdgcn_s_barrier();
+  };
+
+  // ---- operands of 32 rows: tile t, half t & 1 of stage t / 2
+  const int k_at = A::place(c32, h);  // (piece 2 ks + h: the swap moves bit 0 alone)
+  const int i16 = lane & 15, half16 = (lane >> 4) & 1;
+  const int v_at = A::place(4 * h + (i16 >> 2), 2 * half16 + ((i16 & 3) >> 1)) + 8 * (i16 & 1);
+  auto slot_of = [&](int t) { return ring + ((t >> 1) % A::kDepth) * A::kSlot + (t & 1) * 32 * A::kRowB; };
+  auto load_k = [&](bf16x8 (&a)[NK], int t) {
+    const unsigned char* p = slot_of(t) + k_at;
+#pragma unroll
+    for (int k = 0; k < NK; ++k) a[k] = *reinterpret_cast<const bf16x8*>(p + k * 128);
+  };
+  auto load_v = [&](bf16x8 (&a)[2], int t, int cb) {
+    const unsigned char* p = slot_of(t) + A::kSlotK + v_at;
+#pragma unroll
+    for (int m = 0; m < 2; ++m) {
+      union { s16x4 s[2]; bf16x8 b; } x;
+#pragma unroll
+      for (int e = 0; e < 2; ++e)
+        x.s[e] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+            (__attribute__((address_space(3))) s16x4*)(__attribute__((address_space(3))) void*)(p + (4 * m + 2 * e) * (4 * A::kRowB) + cb * 256));
+      a[m] = x.b;
+    }
+  };
+  constexpr float kLimit = 8.f;
+  f32x16 acc[CB], s[2];  // s[t & 1]: logits of tile t
+  bf16x8 p[2][2];        // p[t & 1]: weights of tile t
+  float ref = 0.f, l = 0.f;
+  float limit = kNegInf;            // how far an exponent may lie above the reference: -inf before the first that is seen
+  uint32_t marks[(CB + 1) / 2];     // results that are NaN because their query sees a value that is not finite
+#pragma unroll
+  for (int cb = 0; cb < CB; ++cb) {
+    marks[cb / 2] = 0u;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) acc[cb][i] = 0.f;
+  }
+  auto row_of = [&](int t) { return stage_row(t >> 1) + (t & 1) * 32; };
+  auto aux_of = [&](int t, int what) { return aux_all + ((t >> 1) % A::kDepth) * A::kAux + what * A::kStage + (t & 1) * 32 + 4 * h; };
+  // some query of the wave does not see some row of the tile, though the row is there
+  auto edge = [&](int t) {
+    const int r = row_of(t);
+    return (kp.causal && r + 31 > w_lo) || (pa.window > 0 && r <= w_hi - pa.window && r + 32 > pa.sinks);
+  };
+  auto sees = [&](int t, int i, float bias) {
+    const int r = row_of(t) + (i & 3) + 8 * (i >> 2) + 4 * h;
+    return bias != kNegInf && (!kp.causal || r <= qi) && (pa.window <= 0 || r > qi - pa.window || r < pa.sinks);
+  };
+  auto logits = [&](f32x16& o, const bf16x8 (&a)[NK]) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[i] = 0.f;
+#pragma unroll
+    for (int k = 0; k < NK; ++k) o = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[k], q[k], o, 0, 0, 0);
+  };
+  auto values = [&](const bf16x8 (&a)[2], const bf16x8 (&w)[2], int cb) {
+#pragma unroll
+    for (int m = 0; m < 2; ++m) acc[cb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[m], w[m], acc[cb], 0, 0, 0);
+  };
+  // A tile that some query does not see whole: values that are not finite out of the product, and marks for those
+  // that see one.  (Bits 0 and 16 of not_finite: the halves of a word are no finite numbers.  Whole words at a time:
+  // a predicate for every value would not fit the scalar registers.)
+  auto not_finite = [](uint32_t w) { return (((w & 0x7f807f80u) + 0x00800080u) & 0x80008000u) >> 15; };
+  auto clean = [&](bf16x8 (&a)[2], int t, int cb) {
+    uint32_t odd = 0u;
+#pragma unroll
+    for (int m = 0; m < 2; ++m)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) odd |= not_finite(__builtin_bit_cast(u32x4, a[m])[e]);
+    if (!__any(odd != 0u)) return;
+    const float* bias = aux_of(t, 0);
+    f32x16 seen;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) seen[i] = 0.f;
+#pragma unroll
+    for (int m = 0; m < 2; ++m) {
+      bf16x8 see8;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) see8[e] = (__bf16)(sees(t, 8 * m + e, bias[(e & 3) + 8 * (2 * m + (e >> 2))]) ? 1.f : 0.f);
+      u32x4 w = __builtin_bit_cast(u32x4, a[m]), bad;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const uint32_t n = not_finite(w[e]);
+        bad[e] = n * 0x3f80u;  // one or zero
+        w[e] &= ~(n * 0xffffu);
+      }
+      a[m] = __builtin_bit_cast(bf16x8, w);
+      seen = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, bad), see8, seen, 0, 0, 0);
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) marks[cb / 2] |= min(__float_as_uint(seen[i]), 1u) << (16 * (cb & 1) + i);
+  };
+  auto values_of = [&](int t, const bf16x8 (&w)[2], bool at_edge) {
+#pragma unroll
+    for (int cb = 0; cb < CB; ++cb) {
+      bf16x8 a[2];
+      load_v(a, t, cb);
+      if (at_edge) clean(a, t, cb);
+      values(a, w, cb);
+    }
+  };
+  // Exponents of tile t, in place of its logits, and whether some query's have outgrown its reference (or are the
+  // first that it sees).  PLAIN: every query sees every row, all counts are one.
+  auto exponents = [&](auto plain, int t, f32x16& x, float& mx) {
+    constexpr bool PLAIN = decltype(plain)::value;
+#pragma unroll
+    for (int i4 = 0; i4 < 4; ++i4) {
+      f32x4 ck = {c, c, c, c}, bias;
+      if constexpr (E4M3) ck = *reinterpret_cast<const f32x4*>(aux_of(t, 1) + 8 * i4);
+      if constexpr (!PLAIN) bias = *reinterpret_cast<const f32x4*>(aux_of(t, 0) + 8 * i4);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int i = 4 * i4 + e;
+        if constexpr (PLAIN) x[i] = __builtin_fmaf(x[i], ck[e], -ref);
+        else x[i] = sees(t, i, bias[e]) ? __builtin_fmaf(x[i], ck[e], bias[e] - ref) : kNegInf;
+      }
+    }
+    mx = x[0];
+#pragma unroll
+    for (int i = 1; i < 16; ++i) mx = fmaxf(mx, x[i]);
+    return __any(mx > limit) != 0;
+  };
+  // The reference follows; the result is what the sums so far are to be multiplied with.
+  auto follow = [&](f32x16& x, float mx) {
+    const u32x2 both = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false));
+    const float top = fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1]));
+    const float d = top > limit ? top : 0.f;
+    const float corr = limit == kNegInf ? 1.f : __builtin_amdgcn_exp2f(-d);
+    if (top > limit) limit = kLimit;
+    ref += d;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x[i] -= d;
+    return corr;
+  };
+  auto rescale = [&](float corr) {
+    l *= corr;
+#pragma unroll
+    for (int cb = 0; cb < CB; ++cb)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) acc[cb][i] *= corr;
+  };
+  // Weights from exponents, and their sum.
+  auto weights = [&](auto plain, int t, const f32x16& x, bf16x8 (&w)[2]) {
+    constexpr bool PLAIN = decltype(plain)::value;
+    float sum = 0.f;
+#pragma unroll
+    for (int i4 = 0; i4 < 4; ++i4) {
+      f32x4 vs;
+      if constexpr (E4M3) vs = *reinterpret_cast<const f32x4*>(aux_of(t, 2) + 8 * i4);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int i = 4 * i4 + e;
+        float y = __builtin_amdgcn_exp2f(x[i]);
+        sum += y;
+        if constexpr (E4M3) y = PLAIN || y != 0.f ? y * vs[e] : 0.f;  // (the scale of a row that is not there may be anything)
+        w[i / 8][i % 8] = (__bf16)y;
+      }
+    }
+    return sum;
+  };
+
+  if (n_stages > 0) {
+    issue(0);
+    commit(0);
+    issue(1);
+    commit(1);
+    meet();
+    const int n_tiles = 2 * n_stages;
+    {
+      bf16x8 a[NK];
+      load_k(a, 0);
+      logits(s[0], a);
+    }
+    bool edge_prev = false;
+    for (int st = 0; st < n_stages; ++st) {
+      if (st > 0) meet();
+      issue(st + 2);
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        const int t = 2 * st + half;
+        const int* flags = flag_all + (st % A::kDepth) * 8 + half * 4;
+        const bool at_edge = edge(t);
+        const bool special = __builtin_amdgcn_readfirstlane(flags[0] | flags[1] | flags[2] | flags[3]) || at_edge;
+        float ps, mx, corr = 1.f;
+        bool grown;
+        if (!special && !edge_prev && t > 0 && t + 1 < n_tiles) {
+          bf16x8 a[NK], v[CB][2];
+          load_k(a, t + 1);
+#pragma unroll
+          for (int cb = 0; cb < CB; ++cb) load_v(v[cb], t - 1, cb);
+          logits(s[half ^ 1], a);
+          grown = exponents(std::integral_constant<bool, true>{}, t, s[half], mx);
+          if (grown) corr = follow(s[half], mx);
+#pragma unroll
+          for (int cb = 0; cb < CB; ++cb) values(v[cb], p[half ^ 1], cb);
+          ps = weights(std::integral_constant<bool, true>{}, t, s[half], p[half]);
+          asm volatile("; every row seen");  // (or the compiler shares the end of both branches, and parts the products from the vector work)
+        } else {
+          if (t + 1 < n_tiles) {
+            bf16x8 a[NK];
+            load_k(a, t + 1);
+            logits(s[half ^ 1], a);
+          }
+          grown = exponents(std::integral_constant<bool, false>{}, t, s[half], mx);
+          if (grown) corr = follow(s[half], mx);
+          if (t > 0) values_of(t - 1, p[half ^ 1], edge_prev);
+          ps = weights(std::integral_constant<bool, false>{}, t, s[half], p[half]);
+          asm volatile("; with a mask");
+        }
+        if (grown) rescale(corr);
+        l += ps;
+        edge_prev = at_edge;
+      }
+      commit(st + 2);
+    }
+    values_of(n_tiles - 1, p[1], edge_prev);
+#pragma unroll
+    for (int cb = 0; cb < CB; ++cb)
+#pragma unroll
+      for (int i = 0; i < 16; ++i)  // (all ones: a NaN)
+        acc[cb][i] = __uint_as_float(__float_as_uint(acc[cb][i]) | (uint32_t)((int32_t)(marks[cb / 2] << (31 - (16 * (cb & 1) + i))) >> 31));
+  }
+
+  const u32x2 both = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false));
+  const float den = __uint_as_float(both[0]) + __uint_as_float(both[1]);
+  const int m = w0 + c32;
+  if (m >= m1) return;
+  if (pa.splits == 1) {
+    const int64_t at = array_row(pa.rw, ur.first, m / G);
+    if (at < 0) return;
+    const float inv = den == 0.f ? 1.f : 1.f / den;   // (nothing seen: the sums are zero)
+    uint16_t* o = static_cast<uint16_t*>(pa.out) + (at * G + m % G) * D + 4 * h;
+#pragma unroll
+    for (int cb = 0; cb < CB; ++cb)
+#pragma unroll
+      for (int i4 = 0; i4 < 4; ++i4) {
+        u32x2 w;
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+          w[e] = (uint32_t)float_to_bf16_bits(acc[cb][4 * i4 + 2 * e] * inv) | (uint32_t)float_to_bf16_bits(acc[cb][4 * i4 + 2 * e + 1] * inv) << 16;
+        *reinterpret_cast<u32x2*>(o + cb * 32 + 8 * i4) = w;
+      }
+  } else {
+    float* pp = pa.part + (((int64_t)u * pa.rw.max_n * G + m) * pa.splits + sp) * (D + 2);
+#pragma unroll
+    for (int cb = 0; cb < CB; ++cb)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) pp[cb * 32 + (i & 3) + 8 * (i >> 2) + 4 * h] = acc[cb][i];
+    if (h == 0) {
+      pp[D] = limit == kNegInf ? kNegInf : ref;
+      pp[D + 1] = den;
+    }
+  }
+}
+
+template <bool E4M3, int D>
+hipError_t launch_chunk(const KParams& kp, const PagedAttend& pa, hipStream_t st) {
+  using A = ChunkGeom<D>;
+  const int q_blocks = (int)(((int64_t)pa.rw.max_n * kp.G + A::kBlockQ - 1) / A::kBlockQ);
+  static LdsLimitOnce lim;
+  const hipError_t e = lim.ensure(reinterpret_cast<const void*>(&paged_chunk_kernel<E4M3, D>), 160 * 1024);
+  if (e != hipSuccess) return e;
+  paged_chunk_kernel<E4M3, D><<<dim3(mapped_blocks(pa.pg.n_units, q_blocks * pa.splits)), dim3(512), A::kLds, st>>>(ChunkParams{kp.G, kp.causal, kp.scale_log2}, pa, q_blocks);
+  return hipSuccess;
+}
+
 template <typename T, bool E4M3, int D, int NQ, int WAVES>
 hipError_t launch_rows(const KParams& kp, const PagedAttend& pa, hipStream_t st) {
   const int q_blocks = (int)(((int64_t)pa.rw.max_n * kp.G + NQ * kCols - 1) / (NQ * kCols));
@@ -534,6 +962,11 @@ hipError_t launch_rows(const KParams& kp, const PagedAttend& pa, hipStream_t st)
   const hipError_t e = lim.ensure(reinterpret_cast<const void*>(&paged_rows_kernel<T, E4M3, D, NQ, WAVES>), 160 * 1024);
   if (e != hipSuccess) return e;
   paged_rows_kernel<T, E4M3, D, NQ, WAVES><<<dim3(mapped_blocks(pa.pg.n_units, q_blocks * pa.splits)), dim3(WAVES * 64), lds, st>>>(kp, pa, q_blocks);
+  return hipSuccess;
+}
+
+template <typename T, int D>
+hipError_t launch_combine(const KParams& kp, const PagedAttend& pa, hipStream_t st) {
   if (pa.splits > 1) {
     const int64_t rows = (int64_t)pa.pg.n_units * pa.rw.max_n * kp.G;
     paged_combine_kernel<T, D><<<dim3((unsigned)((rows + 256 / D - 1) / (256 / D))), dim3(256), 0, st>>>(kp.G, pa);
@@ -541,15 +974,19 @@ hipError_t launch_rows(const KParams& kp, const PagedAttend& pa, hipStream_t st)
   return hipGetLastError();
 }
 
+bool chunk_fits(const KParams& kp, int max_n) { return kp.dtype == CASK_BF16 && (int64_t)max_n * kp.G > 64; }
+
 }  // namespace
 
 int paged_splits(const KParams& kp, int n_units, int max_n, bool e4m3, int window, int sinks, int max_rows) {
   (void)e4m3;
-  const int64_t blocks = (int64_t)n_units * (((int64_t)max_n * kp.G + kCols - 1) / kCols);
+  const bool chunk = chunk_fits(kp, max_n);
+  const int64_t per_block = chunk ? ChunkGeom<128>::kBlockQ : kCols;
+  const int64_t blocks = (int64_t)n_units * (((int64_t)max_n * kp.G + per_block - 1) / per_block);
   int64_t rows = max_rows;
   if (window > 0) rows = rows < (int64_t)window + max_n + sinks ? rows : (int64_t)window + max_n + sinks;
-  const int tile = kp.dtype == CASK_BF16 ? 32 : 16;
-  const int rounds = (int)((rows + tile * 8 - 1) / (tile * 8));
+  const int tile = chunk ? 64 : (kp.dtype == CASK_BF16 ? 32 : 16) * 8;
+  const int rounds = (int)((rows + tile - 1) / tile);
   if (blocks > 128 || rounds < 4) return 1;
   int s = (int)(256 / blocks);
   if (s > rounds / 2) s = rounds / 2;
@@ -561,13 +998,22 @@ size_t paged_part_bytes(const KParams& kp, int n_units, int max_n, int splits) {
 }
 
 hipError_t launch_attend_paged(const KParams& kp, const PagedAttend& pa, bool e4m3, hipStream_t st) {
-#define CASK_PA(T, D) return e4m3 ? launch_rows<T, true, D, 1, 8>(kp, pa, st) : launch_rows<T, false, D, 1, 8>(kp, pa, st)
-  if (kp.dtype == CASK_F32) {
-    if (kp.d == 64) CASK_PA(float, 64); else CASK_PA(float, 128);
+  hipError_t e;
+  if (chunk_fits(kp, pa.rw.max_n)) {
+    if (kp.d == 64) e = e4m3 ? launch_chunk<true, 64>(kp, pa, st) : launch_chunk<false, 64>(kp, pa, st);
+    else e = e4m3 ? launch_chunk<true, 128>(kp, pa, st) : launch_chunk<false, 128>(kp, pa, st);
   } else {
-    if (kp.d == 64) CASK_PA(uint16_t, 64); else CASK_PA(uint16_t, 128);
-  }
+#define CASK_PA(T, D) e = e4m3 ? launch_rows<T, true, D, 1, 8>(kp, pa, st) : launch_rows<T, false, D, 1, 8>(kp, pa, st)
+    if (kp.dtype == CASK_F32) {
+      if (kp.d == 64) CASK_PA(float, 64); else CASK_PA(float, 128);
+    } else {
+      if (kp.d == 64) CASK_PA(uint16_t, 64); else CASK_PA(uint16_t, 128);
+    }
 #undef CASK_PA
+  }
+  if (e != hipSuccess) return e;
+  if (kp.dtype == CASK_F32) return kp.d == 64 ? launch_combine<float, 64>(kp, pa, st) : launch_combine<float, 128>(kp, pa, st);
+  return kp.d == 64 ? launch_combine<uint16_t, 64>(kp, pa, st) : launch_combine<uint16_t, 128>(kp, pa, st);
 }
 
 }  // namespace cask
