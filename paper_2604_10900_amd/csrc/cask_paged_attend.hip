@@ -629,7 +629,7 @@ __global__ __launch_bounds__(512, 2) void paged_chunk_kernel(ChunkParams kp, Pag
     const int64_t row = pool_of(s);
     const int r = my_row(s);
     const __amdgpu_buffer_rsrc_t rk = rsrc_of(pa.pg.K, row, r), rv = rsrc_of(pa.pg.V, row, r);
-    unsigned char* slot = ring + (s % A::kDepth) * A::kSlot + wv * 8 * A::kRowB;
+    unsigned char* slot = ring + (s & (A::kDepth - 1)) * A::kSlot + wv * 8 * A::kRowB;
     if constexpr (!E4M3) {
 #pragma unroll
       for (int j = 0; j < kLoads; ++j) {
@@ -646,6 +646,7 @@ __global__ __launch_bounds__(512, 2) void paged_chunk_kernel(ChunkParams kp, Pag
       ev = __builtin_amdgcn_raw_buffer_load_b128(rv, lane * 16, 0, 0);
     }
     a_bias = kNegInf;
+    a_ks = a_vs = 0.f;
     const int mine = r + (lane & 7);
     if (row >= 0 && mine < ur.end) {
       a_bias = 0.f;
@@ -657,20 +658,22 @@ __global__ __launch_bounds__(512, 2) void paged_chunk_kernel(ChunkParams kp, Pag
     }
   };
   auto commit = [&](int s) {  // what came through registers, into the slot
-    float* aux = aux_all + (s % A::kDepth) * A::kAux + wv * 8;
+    float* aux = aux_all + (s & (A::kDepth - 1)) * A::kAux + wv * 8;
     const float bias = a_bias > 1.f ? __log2f(a_bias) : (a_bias == kNegInf ? kNegInf : 0.f);
     if (lane < 8) {
       aux[lane] = bias;
       if constexpr (E4M3) {
         aux[A::kStage + lane] = a_ks * c;
-        aux[2 * A::kStage + lane] = a_vs;
+        aux[2 * A::kStage + lane] = fabsf(a_vs) < __builtin_inff() ? a_vs : 0.f;
       }
     }
     const int f = __any(bias != 0.f);
-    if (lane == 0) flag_all[(s % A::kDepth) * 8 + wv] = f;
+    if (lane == 0) flag_all[(s & (A::kDepth - 1)) * 8 + wv] = f;
     if constexpr (E4M3) {
-      unsigned char* slot = ring + (s % A::kDepth) * A::kSlot;
+      unsigned char* slot = ring + (s & (A::kDepth - 1)) * A::kSlot;
       const int r = wv * 8 + lane / kLanesPerRow, piece = (lane % kLanesPerRow) * 2;
+      // a row of values whose scale is not finite lies there as a row of NaN with a scale of zero
+      const bool lost = !(fabsf(__shfl(a_vs, lane / kLanesPerRow, 64)) < __builtin_inff());
       if (lane < kE4Lanes) {
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
@@ -678,7 +681,7 @@ __global__ __launch_bounds__(512, 2) void paged_chunk_kernel(ChunkParams kp, Pag
 #pragma unroll
           for (int w = 0; w < 4; ++w) {
             k[w] = e4m3_to_bf16(ek[2 * e + w / 2], w & 1);
-            v[w] = e4m3_to_bf16(ev[2 * e + w / 2], w & 1);
+            v[w] = lost ? 0x7fc07fc0u : e4m3_to_bf16(ev[2 * e + w / 2], w & 1);
           }
           *reinterpret_cast<u32x4*>(slot + A::place(r, piece + e)) = k;
           *reinterpret_cast<u32x4*>(slot + A::kSlotK + A::place(r, piece + e)) = v;
@@ -696,7 +699,7 @@ __global__ __launch_bounds__(512, 2) void paged_chunk_kernel(ChunkParams kp, Pag
   const int k_at = A::place(c32, h);  // (piece 2 ks + h: the swap moves bit 0 alone)
   const int i16 = lane & 15, half16 = (lane >> 4) & 1;
   const int v_at = A::place(4 * h + (i16 >> 2), 2 * half16 + ((i16 & 3) >> 1)) + 8 * (i16 & 1);
-  auto slot_of = [&](int t) { return ring + ((t >> 1) % A::kDepth) * A::kSlot + (t & 1) * 32 * A::kRowB; };
+  auto slot_of = [&](int t) { return ring + ((t >> 1) & (A::kDepth - 1)) * A::kSlot + (t & 1) * 32 * A::kRowB; };
   auto load_k = [&](bf16x8 (&a)[NK], int t) {
     const unsigned char* p = slot_of(t) + k_at;
 #pragma unroll
@@ -727,16 +730,22 @@ __global__ __launch_bounds__(512, 2) void paged_chunk_kernel(ChunkParams kp, Pag
     for (int i = 0; i < 16; ++i) acc[cb][i] = 0.f;
   }
   auto row_of = [&](int t) { return stage_row(t >> 1) + (t & 1) * 32; };
-  auto aux_of = [&](int t, int what) { return aux_all + ((t >> 1) % A::kDepth) * A::kAux + what * A::kStage + (t & 1) * 32 + 4 * h; };
+  auto aux_of = [&](int t, int what) { return aux_all + ((t >> 1) & (A::kDepth - 1)) * A::kAux + what * A::kStage + (t & 1) * 32 + 4 * h; };
   // some query of the wave does not see some row of the tile, though the row is there
   auto edge = [&](int t) {
     const int r = row_of(t);
     return (kp.causal && r + 31 > w_lo) || (pa.window > 0 && r <= w_hi - pa.window && r + 32 > pa.sinks);
   };
-  auto sees = [&](int t, int i, float bias) {
-    const int r = row_of(t) + (i & 3) + 8 * (i >> 2) + 4 * h;
-    return bias != kNegInf && (!kp.causal || r <= qi) && (pa.window <= 0 || r > qi - pa.window || r < pa.sinks);
+  // Bit (i & 3) + 8 (i >> 2): the lane's query sees the row of its element i, as far as places go.  (Bits, and masks
+  // made of them, where a predicate for every element would not fit the scalar registers.)
+  auto seen_bits = [&](int t) {
+    const int r = row_of(t);
+    auto below = [](int n) { return n <= 0 ? 0u : (n >= 32 ? ~0u : (1u << n) - 1u); };  // rows r .. r + n - 1
+    uint32_t bits = kp.causal ? below(qi + 1 - r) : ~0u;
+    if (pa.window > 0) bits &= ~below(qi + 1 - pa.window - r) | below(pa.sinks - r);
+    return bits >> (4 * h);
   };
+  auto bit_mask = [](uint32_t bits, int i) { return (uint32_t)((int32_t)(bits << (31 - ((i & 3) + 8 * (i >> 2)))) >> 31); };
   auto logits = [&](f32x16& o, const bf16x8 (&a)[NK]) {
 #pragma unroll
     for (int i = 0; i < 16; ++i) o[i] = 0.f;
@@ -751,22 +760,22 @@ __global__ __launch_bounds__(512, 2) void paged_chunk_kernel(ChunkParams kp, Pag
   // that see one.  (Bits 0 and 16 of not_finite: the halves of a word are no finite numbers.  Whole words at a time:
   // a predicate for every value would not fit the scalar registers.)
   auto not_finite = [](uint32_t w) { return (((w & 0x7f807f80u) + 0x00800080u) & 0x80008000u) >> 15; };
-  auto clean = [&](bf16x8 (&a)[2], int t, int cb) {
+  auto clean = [&](bf16x8 (&a)[2], int t, int cb) {  // (t -1: in front of the first)
     uint32_t odd = 0u;
 #pragma unroll
     for (int m = 0; m < 2; ++m)
 #pragma unroll
       for (int e = 0; e < 4; ++e) odd |= not_finite(__builtin_bit_cast(u32x4, a[m])[e]);
     if (!__any(odd != 0u)) return;
-    const float* bias = aux_of(t, 0);
+    const uint32_t bits = t >= 0 ? seen_bits(t) : 0u;  // (rows that are not there hold zeros)
     f32x16 seen;
 #pragma unroll
     for (int i = 0; i < 16; ++i) seen[i] = 0.f;
 #pragma unroll
     for (int m = 0; m < 2; ++m) {
-      bf16x8 see8;
+      u32x4 see;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) see8[e] = (__bf16)(sees(t, 8 * m + e, bias[(e & 3) + 8 * (2 * m + (e >> 2))]) ? 1.f : 0.f);
+      for (int e = 0; e < 4; ++e) see[e] = (bit_mask(bits, 8 * m + 2 * e) & 0x3f80u) | (bit_mask(bits, 8 * m + 2 * e + 1) & 0x3f800000u);
       u32x4 w = __builtin_bit_cast(u32x4, a[m]), bad;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
@@ -775,40 +784,33 @@ __global__ __launch_bounds__(512, 2) void paged_chunk_kernel(ChunkParams kp, Pag
         w[e] &= ~(n * 0xffffu);
       }
       a[m] = __builtin_bit_cast(bf16x8, w);
-      seen = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, bad), see8, seen, 0, 0, 0);
+      seen = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, bad), __builtin_bit_cast(bf16x8, see), seen, 0, 0, 0);
     }
 #pragma unroll
     for (int i = 0; i < 16; ++i) marks[cb / 2] |= min(__float_as_uint(seen[i]), 1u) << (16 * (cb & 1) + i);
   };
-  auto values_of = [&](int t, const bf16x8 (&w)[2], bool at_edge) {
-#pragma unroll
-    for (int cb = 0; cb < CB; ++cb) {
-      bf16x8 a[2];
-      load_v(a, t, cb);
-      if (at_edge) clean(a, t, cb);
-      values(a, w, cb);
-    }
-  };
-  // Exponents of tile t, in place of its logits, and whether some query's have outgrown its reference (or are the
-  // first that it sees).  PLAIN: every query sees every row, all counts are one.
-  auto exponents = [&](auto plain, int t, f32x16& x, float& mx) {
-    constexpr bool PLAIN = decltype(plain)::value;
+  // Exponents of tile t, in place of its logits ...
+  auto exponents = [&](int t, f32x16& x) {
 #pragma unroll
     for (int i4 = 0; i4 < 4; ++i4) {
-      f32x4 ck = {c, c, c, c}, bias;
+      f32x4 ck = {c, c, c, c};
       if constexpr (E4M3) ck = *reinterpret_cast<const f32x4*>(aux_of(t, 1) + 8 * i4);
-      if constexpr (!PLAIN) bias = *reinterpret_cast<const f32x4*>(aux_of(t, 0) + 8 * i4);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[4 * i4 + e] = __builtin_fmaf(x[4 * i4 + e], ck[e], -ref);
+    }
+  };
+  // ... and where a query does not see every row or a row has a count.
+  auto mask = [&](int t, f32x16& x) {
+    const uint32_t bits = seen_bits(t);
+#pragma unroll
+    for (int i4 = 0; i4 < 4; ++i4) {
+      const f32x4 bias = *reinterpret_cast<const f32x4*>(aux_of(t, 0) + 8 * i4);
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const int i = 4 * i4 + e;
-        if constexpr (PLAIN) x[i] = __builtin_fmaf(x[i], ck[e], -ref);
-        else x[i] = sees(t, i, bias[e]) ? __builtin_fmaf(x[i], ck[e], bias[e] - ref) : kNegInf;
+        const uint32_t m = bit_mask(bits, 4 * i4 + e);
+        x[4 * i4 + e] = __uint_as_float((__float_as_uint(x[4 * i4 + e] + bias[e]) & m) | (__float_as_uint(kNegInf) & ~m));
       }
     }
-    mx = x[0];
-#pragma unroll
-    for (int i = 1; i < 16; ++i) mx = fmaxf(mx, x[i]);
-    return __any(mx > limit) != 0;
   };
   // The reference follows; the result is what the sums so far are to be multiplied with.
   auto follow = [&](f32x16& x, float mx) {
@@ -830,8 +832,7 @@ __global__ __launch_bounds__(512, 2) void paged_chunk_kernel(ChunkParams kp, Pag
       for (int i = 0; i < 16; ++i) acc[cb][i] *= corr;
   };
   // Weights from exponents, and their sum.
-  auto weights = [&](auto plain, int t, const f32x16& x, bf16x8 (&w)[2]) {
-    constexpr bool PLAIN = decltype(plain)::value;
+  auto weights = [&](int t, const f32x16& x, bf16x8 (&w)[2]) {
     float sum = 0.f;
 #pragma unroll
     for (int i4 = 0; i4 < 4; ++i4) {
@@ -839,11 +840,10 @@ __global__ __launch_bounds__(512, 2) void paged_chunk_kernel(ChunkParams kp, Pag
       if constexpr (E4M3) vs = *reinterpret_cast<const f32x4*>(aux_of(t, 2) + 8 * i4);
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const int i = 4 * i4 + e;
-        float y = __builtin_amdgcn_exp2f(x[i]);
+        float y = __builtin_amdgcn_exp2f(x[4 * i4 + e]);
         sum += y;
-        if constexpr (E4M3) y = PLAIN || y != 0.f ? y * vs[e] : 0.f;  // (the scale of a row that is not there may be anything)
-        w[i / 8][i % 8] = (__bf16)y;
+        if constexpr (E4M3) y *= vs[e];  // (finite, see commit: the weight of a row that is not seen stays zero)
+        w[i4 / 2][4 * (i4 % 2) + e] = (__bf16)y;
       }
     }
     return sum;
@@ -855,55 +855,57 @@ __global__ __launch_bounds__(512, 2) void paged_chunk_kernel(ChunkParams kp, Pag
     issue(1);
     commit(1);
     meet();
-    const int n_tiles = 2 * n_stages;
     {
       bf16x8 a[NK];
       load_k(a, 0);
       logits(s[0], a);
     }
-    bool edge_prev = false;
+    // (Turn t: logits of tile t + 1, values of tile t - 1.  Behind the last tile lie zeros; in front of the first,
+    // weights of zero meet the first tile's own values.)
+    bool edge_prev = true;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) p[1][0][e] = p[1][1][e] = (__bf16)0.f;
     for (int st = 0; st < n_stages; ++st) {
       if (st > 0) meet();
       issue(st + 2);
 #pragma unroll
       for (int half = 0; half < 2; ++half) {
         const int t = 2 * st + half;
-        const int* flags = flag_all + (st % A::kDepth) * 8 + half * 4;
+        const int* flags = flag_all + (st & (A::kDepth - 1)) * 8 + half * 4;
         const bool at_edge = edge(t);
         const bool special = __builtin_amdgcn_readfirstlane(flags[0] | flags[1] | flags[2] | flags[3]) || at_edge;
-        float ps, mx, corr = 1.f;
-        bool grown;
-        if (!special && !edge_prev && t > 0 && t + 1 < n_tiles) {
-          bf16x8 a[NK], v[CB][2];
-          load_k(a, t + 1);
+        bf16x8 a[NK], v[CB][2];
+        load_k(a, t + 1);
 #pragma unroll
-          for (int cb = 0; cb < CB; ++cb) load_v(v[cb], t - 1, cb);
-          logits(s[half ^ 1], a);
-          grown = exponents(std::integral_constant<bool, true>{}, t, s[half], mx);
-          if (grown) corr = follow(s[half], mx);
+        for (int cb = 0; cb < CB; ++cb) load_v(v[cb], max(t - 1, 0), cb);
+        logits(s[half ^ 1], a);
+        exponents(t, s[half]);
+        if (special) mask(t, s[half]);
+        float mx = s[half][0], corr = 1.f;
 #pragma unroll
-          for (int cb = 0; cb < CB; ++cb) values(v[cb], p[half ^ 1], cb);
-          ps = weights(std::integral_constant<bool, true>{}, t, s[half], p[half]);
-          asm volatile("; every row seen");  // (or the compiler shares the end of both branches, and parts the products from the vector work)
-        } else {
-          if (t + 1 < n_tiles) {
-            bf16x8 a[NK];
-            load_k(a, t + 1);
-            logits(s[half ^ 1], a);
-          }
-          grown = exponents(std::integral_constant<bool, false>{}, t, s[half], mx);
-          if (grown) corr = follow(s[half], mx);
-          if (t > 0) values_of(t - 1, p[half ^ 1], edge_prev);
-          ps = weights(std::integral_constant<bool, false>{}, t, s[half], p[half]);
-          asm volatile("; with a mask");
-        }
+        for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[half][i]);
+        const bool grown = __any(mx > limit) != 0;  // some query's exponents have outgrown its reference, or are its first
+        if (grown) corr = follow(s[half], mx);
+        if (edge_prev)
+#pragma unroll
+          for (int cb = 0; cb < CB; ++cb) clean(v[cb], t - 1, cb);
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb) values(v[cb], p[half ^ 1], cb);
+        const float ps = weights(t, s[half], p[half]);
         if (grown) rescale(corr);
         l += ps;
         edge_prev = at_edge;
       }
       commit(st + 2);
     }
-    values_of(n_tiles - 1, p[1], edge_prev);
+    const int last = 2 * n_stages - 1;
+#pragma unroll
+    for (int cb = 0; cb < CB; ++cb) {
+      bf16x8 v[2];
+      load_v(v, last, cb);
+      if (edge_prev) clean(v, last, cb);
+      values(v, p[1], cb);
+    }
 #pragma unroll
     for (int cb = 0; cb < CB; ++cb)
 #pragma unroll
