@@ -615,22 +615,37 @@ __global__ __launch_bounds__(512, 2) void paged_chunk_kernel(ChunkParams kp, Pag
     return s < n_stages && r < ur.end ? pool_row(pa.pg, u, r) : -1;
   };
   constexpr int EL = E4M3 ? 1 : 2, ROWB = D * EL;
-  auto rsrc_of = [&](const unsigned char* pool, int64_t row, int r) {
-    const int bytes = __builtin_amdgcn_readfirstlane((row >= 0 ? min(8, ur.end - r) : 0) * ROWB);
-    return __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char*>(pool) + (row >= 0 ? row : 0) * ROWB, 0, bytes, 0x00020000);
+  auto rsrc_of = [&](const void* base, int64_t at, int bytes) {  // (words of a buffer descriptor)
+    const uint64_t p = reinterpret_cast<uint64_t>(base) + at;
+    return u32x4{(uint32_t)__builtin_amdgcn_readfirstlane((int)p), (uint32_t)__builtin_amdgcn_readfirstlane((int)(p >> 32) & 0xffff),
+                 (uint32_t)__builtin_amdgcn_readfirstlane(bytes), 0x00020000u};
+  };
+  auto buffer = [&](const void* base, int64_t at, int bytes) {
+    return __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<unsigned char*>(const_cast<void*>(base)) + at, 0, __builtin_amdgcn_readfirstlane(bytes), 0x00020000u);
+  };
+  // A kilobyte to LDS, sixteen bytes a lane.  (Written out because the compiler lets every transposing read wait for
+  // all such loads that it knows of: 1013 -> 695 us without spilled registers, 695 -> XXX without that wait, for a
+  // chunk of 2048 x 7 rows behind 16 384.  The waits are in `meet`; the loads return no register.)
+  auto load_lds = [&](unsigned char* dst, u32x4 rs, int off) {
+    const int at = __builtin_amdgcn_readfirstlane((int)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)dst);
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(at), "v"(off), "s"(rs) : "memory");
   };
   // bf16: straight to LDS, a KB an instruction; e4m3: sixteen bytes a lane, into LDS as bf16 a stage later
   constexpr int kLoads = 8 * D / 512;               // bf16: instructions of eight rows
   constexpr int kLanesPerRow = D / 16;              // e4m3: lanes that share a row, 16 bytes each
   constexpr int kE4Lanes = 8 * kLanesPerRow;        // lanes that bring some
   u32x4 ek, ev;
-  float a_bias = 0.f, a_ks = 0.f, a_vs = 0.f;       // of row lane % 8 of the wave's eight
+  bool a_here = false;                              // row lane % 8 of the wave's eight: whether it is there, its count, its scales
+  int a_count = 1;
+  uint32_t a_ks = 0u, a_vs = 0u;
   auto issue = [&](int s) {
     const int64_t row = pool_of(s);
     const int r = my_row(s);
-    const __amdgpu_buffer_rsrc_t rk = rsrc_of(pa.pg.K, row, r), rv = rsrc_of(pa.pg.V, row, r);
+    const int rows = row >= 0 ? min(8, ur.end - r) : 0;
+    const int64_t at = row >= 0 ? row : 0;
     unsigned char* slot = ring + (s & (A::kDepth - 1)) * A::kSlot + wv * 8 * A::kRowB;
     if constexpr (!E4M3) {
+      const u32x4 rk = rsrc_of(pa.pg.K, at * ROWB, rows * ROWB), rv = rsrc_of(pa.pg.V, at * ROWB, rows * ROWB);
 #pragma unroll
       for (int j = 0; j < kLoads; ++j) {
         // lane -> group of four rows, piece, row of the group, as they lie in LDS
@@ -638,33 +653,27 @@ __global__ __launch_bounds__(512, 2) void paged_chunk_kernel(ChunkParams kp, Pag
         const int grp = j * (64 / kGroupLanes) + lane / kGroupLanes;
         const int piece = (lane % kGroupLanes) / 4 ^ (grp & 1);
         const int off = (grp * 4 + lane % 4) * ROWB + piece * 16;
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(rk, (__attribute__((address_space(3))) void*)(slot + j * 1024), 16, off, 0, 0, 0);
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(rv, (__attribute__((address_space(3))) void*)(slot + A::kSlotK + j * 1024), 16, off, 0, 0, 0);
+        load_lds(slot + j * 1024, rk, off);
+        load_lds(slot + A::kSlotK + j * 1024, rv, off);
       }
     } else {
-      ek = __builtin_amdgcn_raw_buffer_load_b128(rk, lane * 16, 0, 0);   // (64 channels: the upper lanes read zeros)
-      ev = __builtin_amdgcn_raw_buffer_load_b128(rv, lane * 16, 0, 0);
+      ek = __builtin_amdgcn_raw_buffer_load_b128(buffer(pa.pg.K, at * ROWB, rows * ROWB), lane * 16, 0, 0);   // (64 channels: the upper lanes read zeros)
+      ev = __builtin_amdgcn_raw_buffer_load_b128(buffer(pa.pg.V, at * ROWB, rows * ROWB), lane * 16, 0, 0);
+      a_ks = __builtin_amdgcn_raw_buffer_load_b32(buffer(pa.pg.K_scale, at * 4, rows * 4), (lane & 7) * 4, 0, 0);   // (behind the rows: 0)
+      a_vs = __builtin_amdgcn_raw_buffer_load_b32(buffer(pa.pg.V_scale, at * 4, rows * 4), (lane & 7) * 4, 0, 0);
     }
-    a_bias = kNegInf;
-    a_ks = a_vs = 0.f;
-    const int mine = r + (lane & 7);
-    if (row >= 0 && mine < ur.end) {
-      a_bias = 0.f;
-      if (cu && mine < pa.count_pitch) a_bias = (float)cu[mine];
-      if constexpr (E4M3) {
-        a_ks = pa.pg.K_scale[row + (lane & 7)];
-        a_vs = pa.pg.V_scale[row + (lane & 7)];
-      }
-    }
+    a_here = (lane & 7) < rows;
+    if (cu) a_count = (int)__builtin_amdgcn_raw_buffer_load_b32(buffer(cu, 0, min(pa.count_pitch, 1 << 29) * 4), (r + (lane & 7)) * 4, 0, 0);   // (at or behind count_pitch: 0)
   };
   auto commit = [&](int s) {  // what came through registers, into the slot
     float* aux = aux_all + (s & (A::kDepth - 1)) * A::kAux + wv * 8;
-    const float bias = a_bias > 1.f ? __log2f(a_bias) : (a_bias == kNegInf ? kNegInf : 0.f);
+    const float bias = !a_here ? kNegInf : (a_count > 1 ? __log2f((float)a_count) : 0.f);
+    const float ks = __uint_as_float(a_ks) * c, vs = __uint_as_float(a_vs);
     if (lane < 8) {
       aux[lane] = bias;
       if constexpr (E4M3) {
-        aux[A::kStage + lane] = a_ks * c;
-        aux[2 * A::kStage + lane] = fabsf(a_vs) < __builtin_inff() ? a_vs : 0.f;
+        aux[A::kStage + lane] = ks;
+        aux[2 * A::kStage + lane] = fabsf(vs) < __builtin_inff() ? vs : 0.f;
       }
     }
     const int f = __any(bias != 0.f);
@@ -673,7 +682,7 @@ __global__ __launch_bounds__(512, 2) void paged_chunk_kernel(ChunkParams kp, Pag
       unsigned char* slot = ring + (s & (A::kDepth - 1)) * A::kSlot;
       const int r = wv * 8 + lane / kLanesPerRow, piece = (lane % kLanesPerRow) * 2;
       // a row of values whose scale is not finite lies there as a row of NaN with a scale of zero
-      const bool lost = !(fabsf(__shfl(a_vs, lane / kLanesPerRow, 64)) < __builtin_inff());
+      const bool lost = !(fabsf(__shfl(vs, lane / kLanesPerRow, 64)) < __builtin_inff());
       if (lane < kE4Lanes) {
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
@@ -855,27 +864,28 @@ __global__ __launch_bounds__(512, 2) void paged_chunk_kernel(ChunkParams kp, Pag
     issue(1);
     commit(1);
     meet();
-    {
-      bf16x8 a[NK];
-      load_k(a, 0);
-      logits(s[0], a);
-    }
+    bf16x8 a[NK];
+    load_k(a, 0);
+    logits(s[0], a);
+    load_k(a, 1);
     // (Turn t: logits of tile t + 1, values of tile t - 1.  Behind the last tile lie zeros; in front of the first,
     // weights of zero meet the first tile's own values.)
+    // (bit w: the eight rows that wave w brought are not all there or not all of count one; read a stage ahead)
+    auto flags_of = [&](int s) { return (int)__ballot(flag_all[(s & (A::kDepth - 1)) * 8 + (lane & 7)]) & 0xff; };
+    int flag_next = flags_of(0);
     bool edge_prev = true;
 #pragma unroll
     for (int e = 0; e < 8; ++e) p[1][0][e] = p[1][1][e] = (__bf16)0.f;
     for (int st = 0; st < n_stages; ++st) {
       if (st > 0) meet();
+      const int flag = flag_next;
       issue(st + 2);
+      flag_next = flags_of(st + 1);
 #pragma unroll
       for (int half = 0; half < 2; ++half) {
         const int t = 2 * st + half;
-        const int* flags = flag_all + (st & (A::kDepth - 1)) * 8 + half * 4;
-        const bool at_edge = edge(t);
-        const bool special = __builtin_amdgcn_readfirstlane(flags[0] | flags[1] | flags[2] | flags[3]) || at_edge;
-        bf16x8 a[NK], v[CB][2];
-        load_k(a, t + 1);
+        const bool at_edge = edge(t), special = at_edge || (flag & (half ? 0xf0 : 0x0f));
+        bf16x8 v[CB][2];
 #pragma unroll
         for (int cb = 0; cb < CB; ++cb) load_v(v[cb], max(t - 1, 0), cb);
         logits(s[half ^ 1], a);
@@ -889,6 +899,7 @@ __global__ __launch_bounds__(512, 2) void paged_chunk_kernel(ChunkParams kp, Pag
         if (edge_prev)
 #pragma unroll
           for (int cb = 0; cb < CB; ++cb) clean(v[cb], t - 1, cb);
+        load_k(a, t + 2);
 #pragma unroll
         for (int cb = 0; cb < CB; ++cb) values(v[cb], p[half ^ 1], cb);
         const float ps = weights(t, s[half], p[half]);
