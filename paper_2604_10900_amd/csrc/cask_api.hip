@@ -570,7 +570,7 @@ int cask_attend_paged(const cask_params* params, const cask_pages* pages, const 
   pa.part = static_cast<float*>(ws);
   pa.splits = ws ? paged_splits(kp, pa.pg.n_units, pa.rw.max_n, e4m3, window, sinks, paged_max_rows(pa.pg, max_rows)) : 1;
   if (paged_part_bytes(kp, pa.pg.n_units, pa.rw.max_n, pa.splits) > ws_bytes) pa.splits = 1;
-  return dev_rc(launch_attend_paged(kp, pa, e4m3, static_cast<hipStream_t>(hip_stream)));
+  return dev_rc(launch_attend_paged(kp, pa, e4m3, paged_max_rows(pa.pg, max_rows), static_cast<hipStream_t>(hip_stream)));
 }
 
 size_t cask_attend_paged_workspace_bytes(const cask_params* params, const cask_pages* pages, const cask_rows* rows,

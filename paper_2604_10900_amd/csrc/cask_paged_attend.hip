@@ -77,22 +77,36 @@ template <int WORDS>
 struct Words {
   uint32_t w[WORDS];
 };
-template <int WORDS>
+template <int WORDS, int AUX>
 __device__ inline Words<WORDS> load_words(__amdgpu_buffer_rsrc_t rs, int off, int soff) {
   Words<WORDS> r;
   if constexpr (WORDS == 4) {
-    const u32x4 v = __builtin_amdgcn_raw_buffer_load_b128(rs, off, soff, 0);
+    const u32x4 v = __builtin_amdgcn_raw_buffer_load_b128(rs, off, soff, AUX);
 #pragma unroll
     for (int e = 0; e < 4; ++e) r.w[e] = v[e];
   } else if constexpr (WORDS == 2) {
-    const u32x2 v = __builtin_amdgcn_raw_buffer_load_b64(rs, off, soff, 0);
+    const u32x2 v = __builtin_amdgcn_raw_buffer_load_b64(rs, off, soff, AUX);
     r.w[0] = v[0];
     r.w[1] = v[1];
   } else {
-    r.w[0] = __builtin_amdgcn_raw_buffer_load_b32(rs, off, soff, 0);
+    r.w[0] = __builtin_amdgcn_raw_buffer_load_b32(rs, off, soff, AUX);
   }
   return r;
 }
+
+// Masks as bits and words: a predicate for every element would not fit the scalar registers.
+__device__ inline uint32_t rows_below(int n) { return n <= 0 ? 0u : (n >= 32 ? ~0u : (1u << n) - 1u); }
+// Bit o: the query at row i sees row r + o, as far as places go.
+__device__ inline uint32_t seen_rows(int r, int i, int causal, int window, int sinks) {
+  uint32_t bits = causal ? rows_below(i + 1 - r) : ~0u;
+  if (window > 0) bits &= ~rows_below(i + 1 - window - r) | rows_below(sinks - r);
+  return bits;
+}
+__device__ inline uint32_t bit_mask(uint32_t bits, int b) { return (uint32_t)((int32_t)(bits << (31 - b)) >> 31); }
+__device__ inline float masked(float x, uint32_t m) { return __uint_as_float((__float_as_uint(x) & m) | (__float_as_uint(kNegInf) & ~m)); }
+// 1 where a value is no finite number; of the two bf16 of a word in bits 0 and 16.
+__device__ inline uint32_t not_finite(float x) { return ((__float_as_uint(x) & 0x7fffffffu) + 0x00800000u) >> 31; }
+__device__ inline uint32_t not_finite2(uint32_t w) { return (((w & 0x7f807f80u) + 0x00800080u) & 0x80008000u) >> 15; }
 
 // two e4m3 values of a word as two bf16 in a word (exact)
 __device__ inline uint32_t e4m3_to_bf16(uint32_t w, bool upper) {
@@ -107,6 +121,12 @@ __device__ inline float exp2_from(float x, float reference) { return __builtin_a
 __device__ inline float share(float m, float top) { return m == kNegInf ? 1.f : exp2_from(m, top); }
 // The result of joined sums: zero where no row was seen.
 __device__ inline float joined(float num, float den) { return den == 0.f ? num : num / den; }
+
+// Partial results of the splits: [unit][query row][split] of D sums, behind all of them one reference and one
+// denominator each.
+__device__ inline f32x2* part_state(const PagedAttend& pa, int G, int D) {
+  return reinterpret_cast<f32x2*>(pa.part + (int64_t)pa.pg.n_units * pa.rw.max_n * G * pa.splits * D);
+}
 
 // A wave takes tiles of kTileRows rows of one unit for NQ groups of 16 query rows (token, head): the waves of a
 // workgroup, and the `splits` workgroups that share a block of queries, take them in turn.  Per tile two products
@@ -124,12 +144,13 @@ __device__ inline float joined(float num, float den) { return den == 0.f ? num :
 // which the mask replaces; a value that is not finite would give 0 * inf.  Tiles where the mask hides rows from some
 // queries are looked through for such values; if there are any, they are taken out of the product, and one more
 // product, of zeros and ones, says which results are NaN because a query sees one.
-template <typename T, bool E4M3, int D, int NQ, int WAVES>
-__global__ __launch_bounds__(WAVES * 64) void paged_rows_kernel(KParams kp, PagedAttend pa, int q_blocks) {
+template <typename T, bool E4M3, int D, int NQ, int WAVES, bool NT>
+__global__ __launch_bounds__(WAVES * 64, 8 / WAVES) void paged_rows_kernel(KParams kp, PagedAttend pa, int q_blocks) {
   using A = RowsGeom<T, E4M3, D>;
   constexpr int TR = A::kTileRows, KEYS = A::kKeys, SUB = A::kSub, NB = A::kBlocks, EPV = A::EPV, NV = A::kValLoads;
   constexpr int kAccPitch = D + 4;
   constexpr int ROWB = D * A::kEl;
+  constexpr int kAux = NT ? 2 : 0;  // cache policy of the row loads: non-temporal or default
   extern __shared__ __align__(16) unsigned char rows_lds[];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -174,7 +195,6 @@ __global__ __launch_bounds__(WAVES * 64) void paged_rows_kernel(KParams kp, Page
   Words<A::kValWords> va[KEYS][NV];
   f32x4 ks4[SUB], vs4[SUB];  // scales of the lane's keys
   int cn = 1;
-  bool there[SUB];  // the subtile has a page
   // Subtile y of tile t: its first pool row, -1 where no page is or no row of the unit
   auto sub_row = [&](int t, int y) -> int64_t {
     const int r = t * TR + y * 16;
@@ -196,9 +216,8 @@ __global__ __launch_bounds__(WAVES * 64) void paged_rows_kernel(KParams kp, Page
     for (int y = 0; y < SUB; ++y) {
       const __amdgpu_buffer_rsrc_t rs = sub_rsrc(pa.pg.K, row[y], t, y);
 #pragma unroll
-      for (int i = 0; i < A::kPieces; ++i) ka[y][i] = load_words<A::kPieceWords>(rs, k_off, i * (4 * A::kPieceEl * A::kEl));
+      for (int i = 0; i < A::kPieces; ++i) ka[y][i] = load_words<A::kPieceWords, kAux>(rs, k_off, i * (4 * A::kPieceEl * A::kEl));
       if constexpr (E4M3) ks4[y] = sub_scales(pa.pg.K_scale, row[y]);
-      there[y] = row[y] >= 0;
     }
     if (cu) {
       const int r = t * TR + (lane & (TR - 1));
@@ -214,28 +233,45 @@ __global__ __launch_bounds__(WAVES * 64) void paged_rows_kernel(KParams kp, Page
       for (int j = 0; j < 4; ++j)
 #pragma unroll
         for (int i = 0; i < NV; ++i)
-          va[y * 4 + j][i] = load_words<A::kValWords>(rs, v_off + j * ROWB, i * (16 * EPV * A::kEl));
+          va[y * 4 + j][i] = load_words<A::kValWords, kAux>(rs, v_off + j * ROWB, i * (16 * EPV * A::kEl));
       if constexpr (E4M3) vs4[y] = sub_scales(pa.pg.V_scale, row[y]);
     }
   };
 
   float m_run[NQ], l_run[NQ];
+  uint32_t marks[NQ];  // bit 4 b + r: the result of acc[n][b][r] is NaN
   f32x4 acc[NQ][NB];  // acc[n][b][r] = O[channel(b, 4 g + r)][query n, l16]
 #pragma unroll
   for (int n = 0; n < NQ; ++n) {
     m_run[n] = kNegInf;
     l_run[n] = 0.f;
+    marks[n] = 0u;
 #pragma unroll
     for (int b = 0; b < NB; ++b) acc[n][b] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
 
-  for (int t0 = sp * WAVES + wv; t0 < range.n_tiles; t0 += step) {
-    const int t = range.tile(t0);
-    int64_t row[SUB];
+  // The next tile's keys are requested behind the logits, its values behind the product with the weights, the pages of
+  // the tile after that before both.
+  auto key_mask = [](uint32_t bits, int j) { return bit_mask(bits, (j >> 2) * 16 + (j & 3)); };
+  auto rows_at = [&](int t0, int64_t (&row)[SUB]) {
 #pragma unroll
-    for (int y = 0; y < SUB; ++y) row[y] = sub_row(t, y);
-    load_keys(t, row);
-    load_values(t, row);
+    for (int y = 0; y < SUB; ++y) row[y] = t0 < range.n_tiles ? sub_row(range.tile(t0), y) : -1;
+  };
+  const int t_first = sp * WAVES + wv;
+  int64_t row[SUB], row_next[SUB];
+  rows_at(t_first, row);
+  load_keys(range.tile(t_first), row);
+  load_values(range.tile(t_first), row);
+  rows_at(t_first + step, row_next);
+  for (int t0 = t_first; t0 < range.n_tiles; t0 += step) {
+    const int t = range.tile(t0), t_next = range.tile(t0 + step);
+    bool there[SUB];  // the subtile has a page
+#pragma unroll
+    for (int y = 0; y < SUB; ++y) {
+      there[y] = row[y] >= 0;
+      row[y] = row_next[y];
+    }
+    rows_at(t0 + 2 * step, row_next);
     // Does every query of the block see every row of the tile?
     bool all = t * TR + TR <= ur.end && (!kp.causal || t * TR + TR - 1 <= i_lo);
 #pragma unroll
@@ -284,29 +320,12 @@ __global__ __launch_bounds__(WAVES * 64) void paged_rows_kernel(KParams kp, Page
           }
         }
     }
-    // values that are not finite, in a tile that some query does not see whole
-    bool odd = false;
-    if (!all) {
-      if constexpr (A::kBf16) {
-#pragma unroll
-        for (int b = 0; b < NB; ++b)
-#pragma unroll
-          for (int k2 = 0; k2 < 4; ++k2)
-            odd |= (vb[b][k2] & 0x7f80u) == 0x7f80u || (vb[b][k2] & 0x7f800000u) == 0x7f800000u;
-      } else {
-#pragma unroll
-        for (int j = 0; j < KEYS; ++j)
-#pragma unroll
-          for (int b = 0; b < NB; ++b) odd |= !(fabsf(vf[j][b]) < __builtin_inff());
-      }
-      odd = __any(odd);
-    }
+    f32x4 s[NQ][SUB];
 #pragma unroll
     for (int n = 0; n < NQ; ++n) {
-      f32x4 s[SUB];
 #pragma unroll
       for (int y = 0; y < SUB; ++y) {
-        s[y] = f32x4{0.f, 0.f, 0.f, 0.f};
+        s[n][y] = f32x4{0.f, 0.f, 0.f, 0.f};
         if constexpr (A::kBf16) {
 #pragma unroll
           for (int i = 0; i < A::kPieces; ++i)
@@ -320,8 +339,8 @@ __global__ __launch_bounds__(WAVES * 64) void paged_rows_kernel(KParams kp, Page
 #pragma unroll
                 for (int w = 0; w < 4; ++w) kw[w] = ka[y][i].w[w];
               }
-              s[y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kw),
-                                                             __builtin_bit_cast(bf16x8, q[n][i * A::kPieceQ + e]), s[y], 0, 0, 0);
+              s[n][y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kw),
+                                                             __builtin_bit_cast(bf16x8, q[n][i * A::kPieceQ + e]), s[n][y], 0, 0, 0);
             }
         } else {
           // chains of eight products, the chains in pairs
@@ -350,35 +369,112 @@ __global__ __launch_bounds__(WAVES * 64) void paged_rows_kernel(KParams kp, Page
           for (int o = A::kPieces / 4; o > 0; o >>= 1)
 #pragma unroll
             for (int h = 0; h < o; ++h) chain[h] += chain[h + o];
-          s[y] = chain[0];
+          s[n][y] = chain[0];
         }
-        if constexpr (E4M3) s[y] *= ks4[y];
+        if constexpr (E4M3) s[n][y] *= ks4[y];
       }
-      // s[y][r] = <key 16 y + 4 g + r, query l16>
-      float p[KEYS], mx = kNegInf;
-      bool sees[KEYS];
+    }
+    load_keys(t_next, row);
+    // s[n][y][r] = <key 16 y + 4 g + r, query n, l16>
+    uint32_t bits[NQ];  // bit 16 y + r: the lane's query sees its key of (y, r)
+    if (!all) {
+      uint32_t here = rows_below(ur.end - t * TR);
 #pragma unroll
-      for (int j = 0; j < KEYS; ++j) {
-        sees[j] = true;
-        if (!all) {
-          const int r = t * TR + (j >> 2) * 16 + g * 4 + (j & 3);
-          sees[j] = there[j >> 2] && r < ur.end && (!kp.causal || r <= qi[n]) && (pa.window <= 0 || r > qi[n] - pa.window || r < pa.sinks);
-        }
-        p[j] = sees[j] ? __builtin_fmaf(s[j >> 2][j & 3], c, bias4[j >> 2][j & 3]) : kNegInf;
-        mx = fmaxf(mx, p[j]);
+      for (int y = 0; y < SUB; ++y)
+        if (!there[y]) here &= ~(0xffffu << (16 * y));
+#pragma unroll
+      for (int n = 0; n < NQ; ++n) {
+        bits[n] = (seen_rows(t * TR, qi[n], kp.causal, pa.window, pa.sinks) & here) >> (4 * g);
+        // values that are not finite leave the product; marks stay for those that see one
       }
+      uint32_t odd = 0u;
+      if constexpr (A::kBf16) {
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) odd |= not_finite2(vb[b][e]);
+      } else {
+#pragma unroll
+        for (int j = 0; j < KEYS; ++j)
+#pragma unroll
+          for (int b = 0; b < NB; ++b) odd |= not_finite(vf[j][b]);
+      }
+      if (__any(odd != 0u)) {
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+          f32x4 seen[NQ];
+#pragma unroll
+          for (int n = 0; n < NQ; ++n) seen[n] = f32x4{0.f, 0.f, 0.f, 0.f};
+          if constexpr (A::kBf16) {
+            u32x4 bad;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const uint32_t k = not_finite2(vb[b][e]);
+              bad[e] = k * 0x3f80u;  // one or zero
+              vb[b][e] &= ~(k * 0xffffu);
+            }
+#pragma unroll
+            for (int n = 0; n < NQ; ++n) {
+              u32x4 see;
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                see[e] = (key_mask(bits[n], 2 * e) & 0x3f80u) | (key_mask(bits[n], 2 * e + 1) & 0x3f800000u);
+              seen[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, bad), __builtin_bit_cast(bf16x8, see), seen[n], 0, 0, 0);
+            }
+          } else {
+#pragma unroll
+            for (int j = 0; j < KEYS; ++j) {
+              const uint32_t k = not_finite(vf[j][b]);
+              vf[j][b] = __uint_as_float(__float_as_uint(vf[j][b]) & (k - 1u));
+#pragma unroll
+              for (int n = 0; n < NQ; ++n)
+                seen[n] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(k * 0x3f800000u), __uint_as_float(key_mask(bits[n], j) & 0x3f800000u), seen[n], 0, 0, 0);
+            }
+          }
+#pragma unroll
+          for (int n = 0; n < NQ; ++n)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) marks[n] |= min(__float_as_uint(seen[n][r]), 1u) << (4 * b + r);
+          __builtin_amdgcn_sched_barrier(0);  // (or all blocks' temporaries live at once)
+        }
+      }
+    }
+#pragma unroll
+    for (int n = 0; n < NQ; ++n) {
+      float p[KEYS], mx = kNegInf;
+#pragma unroll
+      for (int j = 0; j < KEYS; ++j) p[j] = __builtin_fmaf(s[n][j >> 2][j & 3], c, bias4[j >> 2][j & 3]);
+      if (!all) {
+#pragma unroll
+        for (int j = 0; j < KEYS; ++j) p[j] = masked(p[j], key_mask(bits[n], j));
+      }
+#pragma unroll
+      for (int j = 0; j < KEYS; ++j) mx = fmaxf(mx, p[j]);
       mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
       mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
       const float mn = fmaxf(m_run[n], mx);
       const float ref = mn == kNegInf ? 0.f : mn;  // (a query that has seen no row yet)
       const float corr = exp2_from(m_run[n], ref);
+      if constexpr (!A::kBf16) {  // (fp32: the logit meets its reference inside one rounding)
+#pragma unroll
+        for (int j = 0; j < KEYS; ++j) p[j] = __builtin_fmaf(s[n][j >> 2][j & 3], c, bias4[j >> 2][j & 3] - ref);
+        if (!all) {
+#pragma unroll
+          for (int j = 0; j < KEYS; ++j) p[j] = masked(p[j], key_mask(bits[n], j));
+        }
+      }
       float ps = 0.f;
 #pragma unroll
       for (int j = 0; j < KEYS; ++j) {
-        if constexpr (A::kBf16) p[j] = exp2_from(p[j], ref);
-        else p[j] = sees[j] ? __builtin_amdgcn_exp2f(__builtin_fmaf(s[j >> 2][j & 3], c, bias4[j >> 2][j & 3] - ref)) : 0.f;  // (the logit meets its reference inside one rounding)
+        p[j] = __builtin_amdgcn_exp2f(A::kBf16 ? p[j] - ref : p[j]);
         ps += p[j];
-        if constexpr (E4M3) p[j] = sees[j] ? p[j] * vs4[j >> 2][j & 3] : 0.f;
+        if constexpr (E4M3) p[j] *= vs4[j >> 2][j & 3];
+      }
+      if constexpr (E4M3) {
+        if (!all) {  // (the scale of a row that is not seen may be anything)
+#pragma unroll
+          for (int j = 0; j < KEYS; ++j) p[j] = __uint_as_float(__float_as_uint(p[j]) & key_mask(bits[n], j));
+        }
       }
       l_run[n] = __builtin_fmaf(l_run[n], corr, ps);
       m_run[n] = mn;
@@ -396,33 +492,10 @@ __global__ __launch_bounds__(WAVES * 64) void paged_rows_kernel(KParams kp, Page
           ph[j] = hi;
           pl[j] = (__bf16)(p[j] - (float)hi);
         }
-        if (!odd) {
 #pragma unroll
-          for (int b = 0; b < NB; ++b) {
-            acc[n][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vb[b]), ph, acc[n][b], 0, 0, 0);
-            acc[n][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vb[b]), pl, acc[n][b], 0, 0, 0);
-          }
-        } else {
-          bf16x8 see8;
-#pragma unroll
-          for (int j = 0; j < 8; ++j) see8[j] = (__bf16)(sees[j] ? 1.f : 0.f);
-#pragma unroll
-          for (int b = 0; b < NB; ++b) {
-            bf16x8 fin, bad;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-              const float x = __uint_as_float(j & 1 ? vb[b][j >> 1] & 0xffff0000u : vb[b][j >> 1] << 16);
-              const bool ok = fabsf(x) < __builtin_inff();
-              fin[j] = (__bf16)(ok ? x : 0.f);
-              bad[j] = (__bf16)(ok ? 0.f : 1.f);
-            }
-            acc[n][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fin, ph, acc[n][b], 0, 0, 0);
-            acc[n][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fin, pl, acc[n][b], 0, 0, 0);
-            const f32x4 seen = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bad, see8, f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-              if (seen[r] > 0.f) acc[n][b][r] = __builtin_nanf("");
-          }
+        for (int b = 0; b < NB; ++b) {
+          acc[n][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vb[b]), ph, acc[n][b], 0, 0, 0);
+          acc[n][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vb[b]), pl, acc[n][b], 0, 0, 0);
         }
       } else {
         // (a tile's products are summed on their own: the long sum has as many addends as there are tiles)
@@ -432,28 +505,14 @@ __global__ __launch_bounds__(WAVES * 64) void paged_rows_kernel(KParams kp, Page
 #pragma unroll
           for (int j = 0; j < KEYS; ++j)
 #pragma unroll
-            for (int b = 0; b < 4; ++b) {
-              float x = vf[j][b0 + b];
-              if (odd) x = fabsf(x) < __builtin_inff() ? x : 0.f;
-              a[b] = __builtin_amdgcn_mfma_f32_16x16x4f32(x, p[j], j ? a[b] : f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
-            }
+            for (int b = 0; b < 4; ++b)
+              a[b] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf[j][b0 + b], p[j], j ? a[b] : f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
 #pragma unroll
           for (int b = 0; b < 4; ++b) acc[n][b0 + b] += a[b];
         }
-        if (odd) {
-#pragma unroll
-          for (int b = 0; b < NB; ++b) {
-            f32x4 seen = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int j = 0; j < KEYS; ++j)
-              seen = __builtin_amdgcn_mfma_f32_16x16x4f32(fabsf(vf[j][b]) < __builtin_inff() ? 0.f : 1.f, sees[j] ? 1.f : 0.f, seen, 0, 0, 0);
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-              if (seen[r] > 0.f) acc[n][b][r] = __builtin_nanf("");
-          }
-        }
       }
     }
+    load_values(t_next, row);
   }
 
   // The waves' states are merged in wave order: the same bits every run.
@@ -468,8 +527,12 @@ __global__ __launch_bounds__(WAVES * 64) void paged_rows_kernel(KParams kp, Page
       st_l[wv * kCols + l16] = l;
     }
 #pragma unroll
-    for (int b = 0; b < NB; ++b)
-      *reinterpret_cast<f32x4*>(&st_acc[(wv * kCols + l16) * kAccPitch + b * 16 + g * 4]) = acc[n][b];
+    for (int b = 0; b < NB; ++b) {
+      f32x4 o = acc[n][b];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) o[r] = __uint_as_float(__float_as_uint(o[r]) | bit_mask(marks[n], 4 * b + r));  // (all ones: a NaN)
+      *reinterpret_cast<f32x4*>(&st_acc[(wv * kCols + l16) * kAccPitch + b * 16 + g * 4]) = o;
+    }
     __syncthreads();
     const int rows_here = min(kCols, m1 - (m0 + n * kCols));
     for (int o = tid; o < rows_here * D; o += WAVES * 64) {
@@ -489,41 +552,59 @@ __global__ __launch_bounds__(WAVES * 64) void paged_rows_kernel(KParams kp, Page
       if (pa.splits == 1) {
         const int64_t row = array_row(pa.rw, ur.first, m / G);
         if (row >= 0) Elem<T>::store(static_cast<T*>(pa.out) + (row * G + m % G) * D + ch, joined(num, den));
-      } else {  // [unit][query row][split]: D sums, then the reference and the denominator
-        float* pp = pa.part + (((int64_t)u * pa.rw.max_n * G + m) * pa.splits + sp) * (D + 2);
-        pp[ch] = num;
-        if (ch == 0) {
-          pp[D] = top;
-          pp[D + 1] = den;
-        }
+      } else {
+        const int64_t at = ((int64_t)u * pa.rw.max_n * G + m) * pa.splits + sp;
+        pa.part[at * D + ch] = num;
+        if (ch == 0) part_state(pa, G, D)[at] = f32x2{top, den};
       }
     }
     __syncthreads();
   }
 }
 
-// Adds the splits of a query row in their order.  D threads per row.
+// Adds the splits of a query row: a wave finds their common reference, a workgroup's 256 / (D / 4) groups of threads
+// take every so many-th of them, the groups' sums are added in order.  (A thread per channel that goes through the
+// splits one by one: 28 rows of 64 splits 20 us.)
 template <typename T, int D>
 __global__ __launch_bounds__(256) void paged_combine_kernel(int G, PagedAttend pa) {
-  const int64_t o = (int64_t)blockIdx.x * (256 / D) + threadIdx.x / D;
-  const int ch = threadIdx.x % D;
-  const int64_t per_unit = (int64_t)pa.rw.max_n * G;
-  if (o >= per_unit * pa.pg.n_units) return;
+  constexpr int kLanes = D / 4, kGroups = 256 / kLanes, kMost = 64;  // (kMost: paged_splits)
+  __shared__ float factor[kMost];
+  __shared__ float total;
+  __shared__ __align__(16) float sums[kGroups][D];
+  const int64_t o = blockIdx.x, per_unit = (int64_t)pa.rw.max_n * G;
   const int u = (int)(o / per_unit), m = (int)(o % per_unit);
   if (m >= rows_of_unit(pa.rw, u) * G) return;
   const int64_t row = array_row(pa.rw, first_of_unit(pa.rw, u), m / G);
   if (row < 0) return;
-  const float* pp = pa.part + o * pa.splits * (D + 2);
-  float mx = kNegInf, num = 0.f, den = 0.f;
-  for (int s = 0; s < pa.splits; ++s) {
-    const float* ps = pp + (int64_t)s * (D + 2);
-    const float pm = ps[D], mn = fmaxf(mx, pm);
-    const float fa = share(mx, mn), fb = share(pm, mn);
-    den = __builtin_fmaf(den, fa, ps[D + 1] * fb);
-    num = __builtin_fmaf(num, fa, ps[ch] * fb);
-    mx = mn;
+  const int S = pa.splits, tid = threadIdx.x, grp = tid / kLanes, ch = (tid % kLanes) * 4;
+  if (tid < 64) {
+    const f32x2 st = tid < S ? part_state(pa, G, D)[o * S + tid] : f32x2{kNegInf, 0.f};
+    float top = st[0];
+#pragma unroll
+    for (int x = 32; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor(top, x, 64));
+    const float f = share(st[0], top);
+    if (tid < S) factor[tid] = f;
+    const float den = wave_sum(tid < S ? st[1] * f : 0.f);
+    if (tid == 0) total = den;
   }
-  Elem<T>::store(static_cast<T*>(pa.out) + (row * G + m % G) * D + ch, joined(num, den));
+  const float* pp = pa.part + o * S * D + ch;
+  f32x4 v[kMost / kGroups];
+#pragma unroll
+  for (int i = 0; i < kMost / kGroups; ++i)
+    v[i] = grp + i * kGroups < S ? *reinterpret_cast<const f32x4*>(pp + (int64_t)(grp + i * kGroups) * D) : f32x4{0.f, 0.f, 0.f, 0.f};
+  __syncthreads();
+  f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int i = 0; i < kMost / kGroups; ++i)
+    if (grp + i * kGroups < S) sum += v[i] * factor[grp + i * kGroups];
+  *reinterpret_cast<f32x4*>(&sums[grp][ch]) = sum;
+  __syncthreads();
+  if (tid < D) {
+    float num = 0.f;
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g) num += sums[g][tid];
+    Elem<T>::store(static_cast<T*>(pa.out) + (row * G + m % G) * D + tid, joined(num, total));
+  }
 }
 
 // ---------------------------------------------------------------- chunks of many query rows
@@ -745,16 +826,9 @@ __global__ __launch_bounds__(512, 2) void paged_chunk_kernel(ChunkParams kp, Pag
     const int r = row_of(t);
     return (kp.causal && r + 31 > w_lo) || (pa.window > 0 && r <= w_hi - pa.window && r + 32 > pa.sinks);
   };
-  // Bit (i & 3) + 8 (i >> 2): the lane's query sees the row of its element i, as far as places go.  (Bits, and masks
-  // made of them, where a predicate for every element would not fit the scalar registers.)
-  auto seen_bits = [&](int t) {
-    const int r = row_of(t);
-    auto below = [](int n) { return n <= 0 ? 0u : (n >= 32 ? ~0u : (1u << n) - 1u); };  // rows r .. r + n - 1
-    uint32_t bits = kp.causal ? below(qi + 1 - r) : ~0u;
-    if (pa.window > 0) bits &= ~below(qi + 1 - pa.window - r) | below(pa.sinks - r);
-    return bits >> (4 * h);
-  };
-  auto bit_mask = [](uint32_t bits, int i) { return (uint32_t)((int32_t)(bits << (31 - ((i & 3) + 8 * (i >> 2)))) >> 31); };
+  // Bit (i & 3) + 8 (i >> 2): the lane's query sees the row of its element i.
+  auto seen_bits = [&](int t) { return seen_rows(row_of(t), qi, kp.causal, pa.window, pa.sinks) >> (4 * h); };
+  auto elem_mask = [](uint32_t bits, int i) { return bit_mask(bits, (i & 3) + 8 * (i >> 2)); };
   auto logits = [&](f32x16& o, const bf16x8 (&a)[NK]) {
 #pragma unroll
     for (int i = 0; i < 16; ++i) o[i] = 0.f;
@@ -766,15 +840,13 @@ __global__ __launch_bounds__(512, 2) void paged_chunk_kernel(ChunkParams kp, Pag
     for (int m = 0; m < 2; ++m) acc[cb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[m], w[m], acc[cb], 0, 0, 0);
   };
   // A tile that some query does not see whole: values that are not finite out of the product, and marks for those
-  // that see one.  (Bits 0 and 16 of not_finite: the halves of a word are no finite numbers.  Whole words at a time:
-  // a predicate for every value would not fit the scalar registers.)
-  auto not_finite = [](uint32_t w) { return (((w & 0x7f807f80u) + 0x00800080u) & 0x80008000u) >> 15; };
+  // that see one.
   auto clean = [&](bf16x8 (&a)[2], int t, int cb) {  // (t -1: in front of the first)
     uint32_t odd = 0u;
 #pragma unroll
     for (int m = 0; m < 2; ++m)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) odd |= not_finite(__builtin_bit_cast(u32x4, a[m])[e]);
+      for (int e = 0; e < 4; ++e) odd |= not_finite2(__builtin_bit_cast(u32x4, a[m])[e]);
     if (!__any(odd != 0u)) return;
     const uint32_t bits = t >= 0 ? seen_bits(t) : 0u;  // (rows that are not there hold zeros)
     f32x16 seen;
@@ -784,11 +856,11 @@ __global__ __launch_bounds__(512, 2) void paged_chunk_kernel(ChunkParams kp, Pag
     for (int m = 0; m < 2; ++m) {
       u32x4 see;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) see[e] = (bit_mask(bits, 8 * m + 2 * e) & 0x3f80u) | (bit_mask(bits, 8 * m + 2 * e + 1) & 0x3f800000u);
+      for (int e = 0; e < 4; ++e) see[e] = (elem_mask(bits, 8 * m + 2 * e) & 0x3f80u) | (elem_mask(bits, 8 * m + 2 * e + 1) & 0x3f800000u);
       u32x4 w = __builtin_bit_cast(u32x4, a[m]), bad;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const uint32_t n = not_finite(w[e]);
+        const uint32_t n = not_finite2(w[e]);
         bad[e] = n * 0x3f80u;  // one or zero
         w[e] &= ~(n * 0xffffu);
       }
@@ -797,6 +869,7 @@ __global__ __launch_bounds__(512, 2) void paged_chunk_kernel(ChunkParams kp, Pag
     }
 #pragma unroll
     for (int i = 0; i < 16; ++i) marks[cb / 2] |= min(__float_as_uint(seen[i]), 1u) << (16 * (cb & 1) + i);
+    __builtin_amdgcn_sched_barrier(0);  // (or all blocks' temporaries live at once)
   };
   // Exponents of tile t, in place of its logits ...
   auto exponents = [&](int t, f32x16& x) {
@@ -815,10 +888,7 @@ __global__ __launch_bounds__(512, 2) void paged_chunk_kernel(ChunkParams kp, Pag
     for (int i4 = 0; i4 < 4; ++i4) {
       const f32x4 bias = *reinterpret_cast<const f32x4*>(aux_of(t, 0) + 8 * i4);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const uint32_t m = bit_mask(bits, 4 * i4 + e);
-        x[4 * i4 + e] = __uint_as_float((__float_as_uint(x[4 * i4 + e] + bias[e]) & m) | (__float_as_uint(kNegInf) & ~m));
-      }
+      for (int e = 0; e < 4; ++e) x[4 * i4 + e] = masked(x[4 * i4 + e] + bias[e], elem_mask(bits, 4 * i4 + e));
     }
   };
   // The reference follows; the result is what the sums so far are to be multiplied with.
@@ -921,7 +991,7 @@ __global__ __launch_bounds__(512, 2) void paged_chunk_kernel(ChunkParams kp, Pag
     for (int cb = 0; cb < CB; ++cb)
 #pragma unroll
       for (int i = 0; i < 16; ++i)  // (all ones: a NaN)
-        acc[cb][i] = __uint_as_float(__float_as_uint(acc[cb][i]) | (uint32_t)((int32_t)(marks[cb / 2] << (31 - (16 * (cb & 1) + i))) >> 31));
+        acc[cb][i] = __uint_as_float(__float_as_uint(acc[cb][i]) | bit_mask(marks[cb / 2], 16 * (cb & 1) + i));
   }
 
   const u32x2 both = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false));
@@ -944,15 +1014,14 @@ __global__ __launch_bounds__(512, 2) void paged_chunk_kernel(ChunkParams kp, Pag
         *reinterpret_cast<u32x2*>(o + cb * 32 + 8 * i4) = w;
       }
   } else {
-    float* pp = pa.part + (((int64_t)u * pa.rw.max_n * G + m) * pa.splits + sp) * (D + 2);
+    const int64_t at = ((int64_t)u * pa.rw.max_n * G + m) * pa.splits + sp;
+    float* pp = pa.part + at * D + 4 * h;
 #pragma unroll
     for (int cb = 0; cb < CB; ++cb)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) pp[cb * 32 + (i & 3) + 8 * (i >> 2) + 4 * h] = acc[cb][i];
-    if (h == 0) {
-      pp[D] = limit == kNegInf ? kNegInf : ref;
-      pp[D + 1] = den;
-    }
+      for (int i4 = 0; i4 < 4; ++i4)
+        *reinterpret_cast<f32x4*>(pp + cb * 32 + 8 * i4) = f32x4{acc[cb][4 * i4], acc[cb][4 * i4 + 1], acc[cb][4 * i4 + 2], acc[cb][4 * i4 + 3]};
+    if (h == 0) part_state(pa, G, D)[at] = f32x2{limit == kNegInf ? kNegInf : ref, den};
   }
 }
 
@@ -967,23 +1036,33 @@ hipError_t launch_chunk(const KParams& kp, const PagedAttend& pa, hipStream_t st
   return hipSuccess;
 }
 
-template <typename T, bool E4M3, int D, int NQ, int WAVES>
-hipError_t launch_rows(const KParams& kp, const PagedAttend& pa, hipStream_t st) {
+template <typename T, bool E4M3, int D, int NQ, int WAVES, bool NT>
+hipError_t launch_rows_as(const KParams& kp, const PagedAttend& pa, hipStream_t st) {
   const int q_blocks = (int)(((int64_t)pa.rw.max_n * kp.G + NQ * kCols - 1) / (NQ * kCols));
   const int lds = WAVES * (32 + 2 * kCols + kCols * (D + 4)) * (int)sizeof(float);
   static LdsLimitOnce lim;  // one per instantiation
-  const hipError_t e = lim.ensure(reinterpret_cast<const void*>(&paged_rows_kernel<T, E4M3, D, NQ, WAVES>), 160 * 1024);
+  const hipError_t e = lim.ensure(reinterpret_cast<const void*>(&paged_rows_kernel<T, E4M3, D, NQ, WAVES, NT>), 160 * 1024);
   if (e != hipSuccess) return e;
-  paged_rows_kernel<T, E4M3, D, NQ, WAVES><<<dim3(mapped_blocks(pa.pg.n_units, q_blocks * pa.splits)), dim3(WAVES * 64), lds, st>>>(kp, pa, q_blocks);
+  paged_rows_kernel<T, E4M3, D, NQ, WAVES, NT><<<dim3(mapped_blocks(pa.pg.n_units, q_blocks * pa.splits)), dim3(WAVES * 64), lds, st>>>(kp, pa, q_blocks);
   return hipSuccess;
+}
+
+template <typename T, bool E4M3, int D>
+hipError_t launch_rows(const KParams& kp, const PagedAttend& pa, int64_t bytes, hipStream_t st) {
+  const int64_t m = (int64_t)pa.rw.max_n * kp.G;
+  constexpr bool kTwo = sizeof(T) == 2 || D == 64;  // (fp32, 128 channels: two groups do not fit the registers)
+  const bool two = kTwo && m > kCols, nt = bytes > (256ll << 20);
+  const int64_t groups = (int64_t)pa.pg.n_units * ((m + (two ? 2 : 1) * kCols - 1) / ((two ? 2 : 1) * kCols)) * pa.splits;
+  auto go = [&](auto f) { return f(kp, pa, st); };
+  if constexpr (kTwo)
+    if (two) return go(&launch_rows_as<T, E4M3, D, 2, 8, false>);
+  if (groups > 256) return nt ? go(&launch_rows_as<T, E4M3, D, 1, 4, true>) : go(&launch_rows_as<T, E4M3, D, 1, 4, false>);
+  return nt ? go(&launch_rows_as<T, E4M3, D, 1, 8, true>) : go(&launch_rows_as<T, E4M3, D, 1, 8, false>);
 }
 
 template <typename T, int D>
 hipError_t launch_combine(const KParams& kp, const PagedAttend& pa, hipStream_t st) {
-  if (pa.splits > 1) {
-    const int64_t rows = (int64_t)pa.pg.n_units * pa.rw.max_n * kp.G;
-    paged_combine_kernel<T, D><<<dim3((unsigned)((rows + 256 / D - 1) / (256 / D))), dim3(256), 0, st>>>(kp.G, pa);
-  }
+  if (pa.splits > 1) paged_combine_kernel<T, D><<<dim3((unsigned)((int64_t)pa.pg.n_units * pa.rw.max_n * kp.G)), dim3(256), 0, st>>>(kp.G, pa);
   return hipGetLastError();
 }
 
@@ -994,7 +1073,7 @@ bool chunk_fits(const KParams& kp, int max_n) { return kp.dtype == CASK_BF16 && 
 int paged_splits(const KParams& kp, int n_units, int max_n, bool e4m3, int window, int sinks, int max_rows) {
   (void)e4m3;
   const bool chunk = chunk_fits(kp, max_n);
-  const int64_t per_block = chunk ? ChunkGeom<128>::kBlockQ : kCols;
+  const int64_t per_block = chunk ? ChunkGeom<128>::kBlockQ : (kp.dtype == CASK_BF16 || kp.d == 64) && (int64_t)max_n * kp.G > kCols ? 2 * kCols : kCols;
   const int64_t blocks = (int64_t)n_units * (((int64_t)max_n * kp.G + per_block - 1) / per_block);
   int64_t rows = max_rows;
   if (window > 0) rows = rows < (int64_t)window + max_n + sinks ? rows : (int64_t)window + max_n + sinks;
@@ -1010,13 +1089,16 @@ size_t paged_part_bytes(const KParams& kp, int n_units, int max_n, int splits) {
   return splits <= 1 ? 0 : (size_t)n_units * max_n * kp.G * splits * (kp.d + 2) * sizeof(float);
 }
 
-hipError_t launch_attend_paged(const KParams& kp, const PagedAttend& pa, bool e4m3, hipStream_t st) {
+hipError_t launch_attend_paged(const KParams& kp, const PagedAttend& pa, bool e4m3, int max_rows, hipStream_t st) {
+  int64_t rows = max_rows;  // what a unit's queries see, at the most
+  if (pa.window > 0 && (int64_t)pa.window + pa.rw.max_n + pa.sinks < rows) rows = (int64_t)pa.window + pa.rw.max_n + pa.sinks;
+  const int64_t bytes = pa.pg.n_units * rows * 2 * kp.d * (e4m3 ? 1 : kp.dtype == CASK_F32 ? 4 : 2);
   hipError_t e;
   if (chunk_fits(kp, pa.rw.max_n)) {
     if (kp.d == 64) e = e4m3 ? launch_chunk<true, 64>(kp, pa, st) : launch_chunk<false, 64>(kp, pa, st);
     else e = e4m3 ? launch_chunk<true, 128>(kp, pa, st) : launch_chunk<false, 128>(kp, pa, st);
   } else {
-#define CASK_PA(T, D) e = e4m3 ? launch_rows<T, true, D, 1, 8>(kp, pa, st) : launch_rows<T, false, D, 1, 8>(kp, pa, st)
+#define CASK_PA(T, D) e = e4m3 ? launch_rows<T, true, D>(kp, pa, bytes, st) : launch_rows<T, false, D>(kp, pa, bytes, st)
     if (kp.dtype == CASK_F32) {
       if (kp.d == 64) CASK_PA(float, 64); else CASK_PA(float, 128);
     } else {
