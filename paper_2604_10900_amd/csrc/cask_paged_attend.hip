@@ -972,7 +972,15 @@ __global__ __launch_bounds__(512, 2) void paged_chunk_kernel(ChunkParams kp, Pag
         load_k(a, t + 2);
 #pragma unroll
         for (int cb = 0; cb < CB; ++cb) values(v[cb], p[half ^ 1], cb);
-        const float ps = weights(t, s[half], p[half]);
+        float ps = weights(t, s[half], p[half]);
+        asm volatile("" : "+v"(ps));  // (or the weights move behind the branch below, away from the products they run beside)
+#pragma unroll
+        for (int k = 0; k < 2 * CB; ++k) {
+          __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);            // a matrix instruction,
+          __builtin_amdgcn_sched_group_barrier(0x100, NK / (2 * CB), 0);  // key reads,
+          __builtin_amdgcn_sched_group_barrier(0x400, 16 / (2 * CB), 0);  // exponentials
+          __builtin_amdgcn_sched_group_barrier(0x002, 24 / (2 * CB) + 1, 0);
+        }
         if (grown) rescale(corr);
         l += ps;
         edge_prev = at_edge;
