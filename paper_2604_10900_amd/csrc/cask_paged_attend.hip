@@ -625,8 +625,8 @@ struct ChunkGeom {
   static constexpr int kSlotK = kStage * kRowB;         // keys of a slot; its values lie behind them
   static constexpr int kSlot = 2 * kSlotK;
   static constexpr int kDepth = 4;
-  static constexpr int kAux = kStage * 3;               // floats of a slot: bias, key scale, value scale of a row
-  static constexpr int kLds = kDepth * (kSlot + kAux * 4 + 32);
+  static constexpr int kAux = kStage * 3;               // words of a slot: count, later its logarithm, key scale, value scale of a row
+  static constexpr int kLds = kDepth * (kSlot + kAux * 4 + 8);
   // Rows lie in LDS in groups of four, the group's 16-byte pieces one behind the other, each of them for its four
   // rows; every other group has its neighbouring pieces swapped.  Eight rows' reads of one piece (keys), and four
   // rows' reads of two neighbouring pieces (values), then meet 128 bytes that lie together.
@@ -652,7 +652,7 @@ __global__ __launch_bounds__(512, 2) void paged_chunk_kernel(ChunkParams kp, Pag
   constexpr int NK = D / 16, CB = D / 32;
   extern __shared__ __align__(16) unsigned char ring[];
   float* aux_all = reinterpret_cast<float*>(ring + A::kDepth * A::kSlot);
-  int* flag_all = reinterpret_cast<int*>(aux_all + A::kDepth * A::kAux);
+  unsigned char* flag_all = reinterpret_cast<unsigned char*>(aux_all + A::kDepth * A::kAux);
   const int tid = threadIdx.x, lane = tid & 63;
   const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int c32 = lane & 31, h = lane >> 5;
@@ -690,13 +690,28 @@ __global__ __launch_bounds__(512, 2) void paged_chunk_kernel(ChunkParams kp, Pag
 
   // ---- the ring: wave wv brings rows [8 wv, 8 wv + 8) of a stage, all of one page
   auto stage_row = [&](int s) { return range.tile(s_begin + s) * A::kStage; };
-  auto my_row = [&](int s) { return stage_row(s) + wv * 8; };
-  auto pool_of = [&](int s) -> int64_t {
-    const int r = my_row(s);
-    return s < n_stages && r < ur.end ? pool_row(pa.pg, u, r) : -1;
-  };
   constexpr int EL = E4M3 ? 1 : 2, ROWB = D * EL;
-  auto rsrc_of = [&](const void* base, int64_t at, int bytes) {  // (words of a buffer descriptor)
+  // Page of the wave's rows of stage 64 k + lane: one load for 64 stages.  (Looked up at its stage, each entry made
+  // the whole wave wait for it.)
+  int entries = -1;
+  auto load_entries = [&](int s0) {
+    const int s = s0 + lane, r = stage_row(s) + wv * 8;
+    entries = -1;
+    if (s < n_stages && r < ur.end) entries = pa.pg.table ? pa.pg.table[(int64_t)u * pa.pg.table_pitch + (r >> pa.pg.shift)] : u;
+  };
+  struct Place {
+    int64_t at;  // pool row of the first of the wave's rows of a stage
+    int rows;    // how many are there
+  };
+  auto find = [&](int s) {
+    const int e = __builtin_amdgcn_readlane(entries, s & 63), r = stage_row(s) + wv * 8;
+    Place p{0, 0};
+    if ((unsigned)e < (unsigned)pa.pg.n_pages) p = Place{e * pa.pg.pitch + (r & pa.pg.mask), min(8, ur.end - r)};
+    // (bit o of a stage's eight bytes: row o of it is there; read by all waves a stage before its own)
+    if (lane == 0) flag_all[(s & (A::kDepth - 1)) * 8 + wv] = (unsigned char)((1 << p.rows) - 1);
+    return p;
+  };
+  auto rsrc_of = [&](const void* base, int64_t at, int bytes) {  // words of a buffer descriptor
     const uint64_t p = reinterpret_cast<uint64_t>(base) + at;
     return u32x4{(uint32_t)__builtin_amdgcn_readfirstlane((int)p), (uint32_t)__builtin_amdgcn_readfirstlane((int)(p >> 32) & 0xffff),
                  (uint32_t)__builtin_amdgcn_readfirstlane(bytes), 0x00020000u};
@@ -704,84 +719,89 @@ __global__ __launch_bounds__(512, 2) void paged_chunk_kernel(ChunkParams kp, Pag
   auto buffer = [&](const void* base, int64_t at, int bytes) {
     return __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<unsigned char*>(const_cast<void*>(base)) + at, 0, __builtin_amdgcn_readfirstlane(bytes), 0x00020000u);
   };
+  auto lds_address = [](const void* p) {
+    return __builtin_amdgcn_readfirstlane((int)(uintptr_t)(__attribute__((address_space(3))) const unsigned char*)p);
+  };
   // A kilobyte to LDS, sixteen bytes a lane.  (Written out because the compiler lets every transposing read wait for
-  // all such loads that it knows of: 1013 -> 695 us without spilled registers, 695 -> XXX without that wait, for a
-  // chunk of 2048 x 7 rows behind 16 384.  The waits are in `meet`; the loads return no register.)
+  // all such loads that it knows of: a chunk of 2048 x 7 query rows behind 16 384 rows took 695 us so and 559 without
+  // that wait.  The waits are in `meet`; the loads return no register.)
   auto load_lds = [&](unsigned char* dst, u32x4 rs, int off) {
-    const int at = __builtin_amdgcn_readfirstlane((int)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)dst);
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(at), "v"(off), "s"(rs) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds_address(dst)), "v"(off), "s"(rs) : "memory");
   };
-  // bf16: straight to LDS, a KB an instruction; e4m3: sixteen bytes a lane, into LDS as bf16 a stage later
-  constexpr int kLoads = 8 * D / 512;               // bf16: instructions of eight rows
-  constexpr int kLanesPerRow = D / 16;              // e4m3: lanes that share a row, 16 bytes each
-  constexpr int kE4Lanes = 8 * kLanesPerRow;        // lanes that bring some
-  u32x4 ek, ev;
-  bool a_here = false;                              // row lane % 8 of the wave's eight: whether it is there, its count, its scales
-  int a_count = 1;
-  uint32_t a_ks = 0u, a_vs = 0u;
-  auto issue = [&](int s) {
-    const int64_t row = pool_of(s);
-    const int r = my_row(s);
-    const int rows = row >= 0 ? min(8, ur.end - r) : 0;
-    const int64_t at = row >= 0 ? row : 0;
-    unsigned char* slot = ring + (s & (A::kDepth - 1)) * A::kSlot + wv * 8 * A::kRowB;
-    if constexpr (!E4M3) {
-      const u32x4 rk = rsrc_of(pa.pg.K, at * ROWB, rows * ROWB), rv = rsrc_of(pa.pg.V, at * ROWB, rows * ROWB);
+  // bf16: straight to LDS, a KB an instruction.  Lane -> group of four rows, piece, row of the group as they lie there.
+  constexpr int kLoads = 8 * D / 512, kGroupLanes = D / 2;   // instructions of eight rows; lanes of a group
+  auto load_rows = [&](unsigned char* dst, const unsigned char* pool, const Place& p) {
+    const u32x4 rs = rsrc_of(pool, p.at * ROWB, p.rows * ROWB);
 #pragma unroll
-      for (int j = 0; j < kLoads; ++j) {
-        // lane -> group of four rows, piece, row of the group, as they lie in LDS
-        constexpr int kPieces = D / 8, kGroupLanes = 4 * kPieces;   // (64 channels: two groups an instruction)
-        const int grp = j * (64 / kGroupLanes) + lane / kGroupLanes;
-        const int piece = (lane % kGroupLanes) / 4 ^ (grp & 1);
-        const int off = (grp * 4 + lane % 4) * ROWB + piece * 16;
-        load_lds(slot + j * 1024, rk, off);
-        load_lds(slot + A::kSlotK + j * 1024, rv, off);
-      }
-    } else {
-      ek = __builtin_amdgcn_raw_buffer_load_b128(buffer(pa.pg.K, at * ROWB, rows * ROWB), lane * 16, 0, 0);   // (64 channels: the upper lanes read zeros)
-      ev = __builtin_amdgcn_raw_buffer_load_b128(buffer(pa.pg.V, at * ROWB, rows * ROWB), lane * 16, 0, 0);
-      a_ks = __builtin_amdgcn_raw_buffer_load_b32(buffer(pa.pg.K_scale, at * 4, rows * 4), (lane & 7) * 4, 0, 0);   // (behind the rows: 0)
-      a_vs = __builtin_amdgcn_raw_buffer_load_b32(buffer(pa.pg.V_scale, at * 4, rows * 4), (lane & 7) * 4, 0, 0);
+    for (int j = 0; j < kLoads; ++j) {
+      const int grp = j * (64 / kGroupLanes) + lane / kGroupLanes;
+      const int piece = (lane % kGroupLanes) / 4 ^ (grp & 1);
+      load_lds(dst + j * 1024, rs, (grp * 4 + lane % 4) * ROWB + piece * 16);
     }
-    a_here = (lane & 7) < rows;
-    if (cu) a_count = (int)__builtin_amdgcn_raw_buffer_load_b32(buffer(cu, 0, min(pa.count_pitch, 1 << 29) * 4), (r + (lane & 7)) * 4, 0, 0);   // (at or behind count_pitch: 0)
   };
-  auto commit = [&](int s) {  // what came through registers, into the slot
+  auto slot_at = [&](int s) { return ring + (s & (A::kDepth - 1)) * A::kSlot; };
+  auto load_counts = [&](int s) {  // of a stage's rows, by one of the waves
+    const int r = stage_row(s);
+    if (!cu || s >= n_stages || r >= pa.count_pitch || wv != (s & 7)) return;
+    const u32x4 rs = rsrc_of(cu, (int64_t)r * 4, min(pa.count_pitch - r, A::kStage) * 4);  // (behind them: 0, which counts as one)
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(lds_address(aux_all + (s & (A::kDepth - 1)) * A::kAux)),
+                 "v"(lane * 4), "s"(rs) : "memory");
+  };
+  // Counts of stage s into their logarithms, a stage before it: by the wave that asked for them, once they are there.
+  auto convert_counts = [&](int s) {
+    if (!cu || s >= n_stages || stage_row(s) >= pa.count_pitch || wv != (s & 7)) return;
+    if constexpr (E4M3) __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): (bf16: `meet` has waited for them)
+    float* at = aux_all + (s & (A::kDepth - 1)) * A::kAux + lane;
+    asm volatile("" ::: "memory");
+    *at = __builtin_amdgcn_logf((float)max((int)__float_as_uint(*at), 1));
+  };
+  auto load_keys = [&](int s, const Place& p) {
+    load_counts(s);
+    load_rows(slot_at(s) + wv * 8 * A::kRowB, pa.pg.K, p);
+  };
+  auto load_values = [&](int s, const Place& p) { load_rows(slot_at(s) + A::kSlotK + wv * 8 * A::kRowB, pa.pg.V, p); };
+  // e4m3: sixteen bytes a lane into registers, a stage later into LDS as bf16
+  constexpr int kLanesPerRow = D / 16;              // lanes that share a row
+  u32x4 ek, ev;
+  uint32_t a_ks = 0u, a_vs = 0u;                    // scales of row lane % 8 of the wave's eight
+  auto issue = [&](int s) {
+    const Place p = find(s);
+    load_counts(s);
+    ek = __builtin_amdgcn_raw_buffer_load_b128(buffer(pa.pg.K, p.at * ROWB, p.rows * ROWB), lane * 16, 0, 0);   // (64 channels: the upper lanes read zeros)
+    ev = __builtin_amdgcn_raw_buffer_load_b128(buffer(pa.pg.V, p.at * ROWB, p.rows * ROWB), lane * 16, 0, 0);
+    a_ks = __builtin_amdgcn_raw_buffer_load_b32(buffer(pa.pg.K_scale, p.at * 4, p.rows * 4), (lane & 7) * 4, 0, 0);   // (behind the rows: 0)
+    a_vs = __builtin_amdgcn_raw_buffer_load_b32(buffer(pa.pg.V_scale, p.at * 4, p.rows * 4), (lane & 7) * 4, 0, 0);
+  };
+  auto commit = [&](int s) {
     float* aux = aux_all + (s & (A::kDepth - 1)) * A::kAux + wv * 8;
-    const float bias = !a_here ? kNegInf : (a_count > 1 ? __log2f((float)a_count) : 0.f);
     const float ks = __uint_as_float(a_ks) * c, vs = __uint_as_float(a_vs);
     if (lane < 8) {
-      aux[lane] = bias;
-      if constexpr (E4M3) {
-        aux[A::kStage + lane] = ks;
-        aux[2 * A::kStage + lane] = fabsf(vs) < __builtin_inff() ? vs : 0.f;
-      }
+      aux[A::kStage + lane] = ks;
+      aux[2 * A::kStage + lane] = fabsf(vs) < __builtin_inff() ? vs : 0.f;
     }
-    const int f = __any(bias != 0.f);
-    if (lane == 0) flag_all[(s & (A::kDepth - 1)) * 8 + wv] = f;
-    if constexpr (E4M3) {
-      unsigned char* slot = ring + (s & (A::kDepth - 1)) * A::kSlot;
-      const int r = wv * 8 + lane / kLanesPerRow, piece = (lane % kLanesPerRow) * 2;
-      // a row of values whose scale is not finite lies there as a row of NaN with a scale of zero
-      const bool lost = !(fabsf(__shfl(vs, lane / kLanesPerRow, 64)) < __builtin_inff());
-      if (lane < kE4Lanes) {
+    convert_counts(s);
+    unsigned char* slot = slot_at(s);
+    const int r = wv * 8 + lane / kLanesPerRow, piece = (lane % kLanesPerRow) * 2;
+    // a row of values whose scale is not finite lies there as a row of NaN with a scale of zero
+    const bool lost = !(fabsf(__shfl(vs, lane / kLanesPerRow, 64)) < __builtin_inff());
+    if (lane < 8 * kLanesPerRow) {
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          u32x4 k, v;
+      for (int e = 0; e < 2; ++e) {
+        u32x4 k, v;
 #pragma unroll
-          for (int w = 0; w < 4; ++w) {
-            k[w] = e4m3_to_bf16(ek[2 * e + w / 2], w & 1);
-            v[w] = lost ? 0x7fc07fc0u : e4m3_to_bf16(ev[2 * e + w / 2], w & 1);
-          }
-          *reinterpret_cast<u32x4*>(slot + A::place(r, piece + e)) = k;
-          *reinterpret_cast<u32x4*>(slot + A::kSlotK + A::place(r, piece + e)) = v;
+        for (int w = 0; w < 4; ++w) {
+          k[w] = e4m3_to_bf16(ek[2 * e + w / 2], w & 1);
+          v[w] = lost ? 0x7fc07fc0u : e4m3_to_bf16(ev[2 * e + w / 2], w & 1);
         }
+        *reinterpret_cast<u32x4*>(slot + A::place(r, piece + e)) = k;
+        *reinterpret_cast<u32x4*>(slot + A::kSlotK + A::place(r, piece + e)) = v;
       }
     }
   };
-  // every wave's share of every stage issued so far has landed, and the slot used before last is free
+  // Between stages: every wave's rows that the next one reads have landed, and it reads none of those that will be
+  // written over.  bf16: the loads of the stage that ends here may still be under way.
   auto meet = [&]() {
-    __builtin_amdgcn_s_waitcnt(0x0070);  // vmcnt(0) lgkmcnt(0)
+    __builtin_amdgcn_s_waitcnt(E4M3 ? 0xc07f : 0x0070 | 2 * kLoads);  // lgkmcnt(0), and vmcnt(2 kLoads)
     __builtin_amdgcn_s_barrier();
   };
 
@@ -821,6 +841,7 @@ __global__ __launch_bounds__(512, 2) void paged_chunk_kernel(ChunkParams kp, Pag
   }
   auto row_of = [&](int t) { return stage_row(t >> 1) + (t & 1) * 32; };
   auto aux_of = [&](int t, int what) { return aux_all + ((t >> 1) & (A::kDepth - 1)) * A::kAux + what * A::kStage + (t & 1) * 32 + 4 * h; };
+  auto counted = [&](int t) { return cu && row_of(t) < pa.count_pitch; };
   // some query of the wave does not see some row of the tile, though the row is there
   auto edge = [&](int t) {
     const int r = row_of(t);
@@ -882,14 +903,18 @@ __global__ __launch_bounds__(512, 2) void paged_chunk_kernel(ChunkParams kp, Pag
     }
   };
   // ... and where a query does not see every row or a row has a count.
-  auto mask = [&](int t, f32x16& x) {
-    const uint32_t bits = seen_bits(t);
+  auto mask = [&](int t, f32x16& x, uint32_t here) {
+    if (counted(t)) {
 #pragma unroll
-    for (int i4 = 0; i4 < 4; ++i4) {
-      const f32x4 bias = *reinterpret_cast<const f32x4*>(aux_of(t, 0) + 8 * i4);
+      for (int i4 = 0; i4 < 4; ++i4) {
+        const f32x4 bias = *reinterpret_cast<const f32x4*>(aux_of(t, 0) + 8 * i4);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) x[4 * i4 + e] = masked(x[4 * i4 + e] + bias[e], elem_mask(bits, 4 * i4 + e));
+        for (int e = 0; e < 4; ++e) x[4 * i4 + e] += bias[e];
+      }
     }
+    const uint32_t bits = seen_bits(t) & (here >> (4 * h));
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x[i] = masked(x[i], elem_mask(bits, i));
   };
   // The reference follows; the result is what the sums so far are to be multiplied with.
   auto follow = [&](f32x16& x, float mx) {
@@ -929,38 +954,61 @@ __global__ __launch_bounds__(512, 2) void paged_chunk_kernel(ChunkParams kp, Pag
   };
 
   if (n_stages > 0) {
-    issue(0);
-    commit(0);
-    issue(1);
-    commit(1);
+    // Keys are requested three stages ahead and values two: turn t reads keys of tile t + 2 and values of tile t - 1.
+    load_entries(0);
+    Place next_v;
+    if constexpr (E4M3) {
+      issue(0);
+      commit(0);
+      issue(1);
+      commit(1);
+      issue(2);
+    } else {
+      const Place p0 = find(0), p1 = find(1);
+      load_keys(0, p0);
+      load_values(0, p0);
+      load_keys(1, p1);
+      next_v = find(2);
+      load_keys(2, next_v);
+      load_values(1, p1);
+    }
     meet();
+    if constexpr (!E4M3) {
+      convert_counts(0);
+      if (counted(0)) meet();
+    }
     bf16x8 a[NK];
     load_k(a, 0);
     logits(s[0], a);
     load_k(a, 1);
-    // (Turn t: logits of tile t + 1, values of tile t - 1.  Behind the last tile lie zeros; in front of the first,
-    // weights of zero meet the first tile's own values.)
-    // (bit w: the eight rows that wave w brought are not all there or not all of count one; read a stage ahead)
-    auto flags_of = [&](int s) { return (int)__ballot(flag_all[(s & (A::kDepth - 1)) * 8 + (lane & 7)]) & 0xff; };
-    int flag_next = flags_of(0);
+    auto flags_of = [&](int s) { return *reinterpret_cast<const u32x2*>(flag_all + (s & (A::kDepth - 1)) * 8); };
+    u32x2 flag_next = flags_of(0);
+    // (Behind the last tile lie zeros; in front of the first, weights of zero meet the first tile's own values.)
     bool edge_prev = true;
 #pragma unroll
     for (int e = 0; e < 8; ++e) p[1][0][e] = p[1][1][e] = (__bf16)0.f;
     for (int st = 0; st < n_stages; ++st) {
       if (st > 0) meet();
-      const int flag = flag_next;
-      issue(st + 2);
+      const uint32_t here[2] = {(uint32_t)__builtin_amdgcn_readfirstlane((int)flag_next[0]), (uint32_t)__builtin_amdgcn_readfirstlane((int)flag_next[1])};
       flag_next = flags_of(st + 1);
+      if (((st + 3) & 63) == 0) load_entries(st + 3);
+      if constexpr (!E4M3) {
+        const Place next_k = find(st + 3);
+        load_keys(st + 3, next_k);
+        load_values(st + 2, next_v);
+        next_v = next_k;
+        convert_counts(st + 1);
+      }
 #pragma unroll
       for (int half = 0; half < 2; ++half) {
         const int t = 2 * st + half;
-        const bool at_edge = edge(t), special = at_edge || (flag & (half ? 0xf0 : 0x0f));
+        const bool at_edge = edge(t), special = at_edge || here[half] != ~0u || counted(t);
         bf16x8 v[CB][2];
 #pragma unroll
         for (int cb = 0; cb < CB; ++cb) load_v(v[cb], max(t - 1, 0), cb);
         logits(s[half ^ 1], a);
         exponents(t, s[half]);
-        if (special) mask(t, s[half]);
+        if (special) mask(t, s[half], here[half]);
         float mx = s[half][0], corr = 1.f;
 #pragma unroll
         for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[half][i]);
@@ -984,8 +1032,12 @@ __global__ __launch_bounds__(512, 2) void paged_chunk_kernel(ChunkParams kp, Pag
         if (grown) rescale(corr);
         l += ps;
         edge_prev = at_edge;
+        if constexpr (E4M3)
+          if (half == 0) {
+            commit(st + 2);
+            issue(st + 3);
+          }
       }
-      commit(st + 2);
     }
     const int last = 2 * n_stages - 1;
 #pragma unroll
