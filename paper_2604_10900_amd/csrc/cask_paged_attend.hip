@@ -809,14 +809,14 @@ __global__ __launch_bounds__(512, 2) void paged_chunk_kernel(ChunkParams kp, Pag
   const int k_at = A::place(c32, h);  // (piece 2 ks + h: the swap moves bit 0 alone)
   const int i16 = lane & 15, half16 = (lane >> 4) & 1;
   const int v_at = A::place(4 * h + (i16 >> 2), 2 * half16 + ((i16 & 3) >> 1)) + 8 * (i16 & 1);
-  auto slot_of = [&](int t) { return ring + ((t >> 1) & (A::kDepth - 1)) * A::kSlot + (t & 1) * 32 * A::kRowB; };
-  auto load_k = [&](bf16x8 (&a)[NK], int t) {
-    const unsigned char* p = slot_of(t) + k_at;
+  // (a tile is named by its stage's place in the ring, in slots, and its half)
+  auto load_k = [&](bf16x8 (&a)[NK], int place, int half) {
+    const unsigned char* p = ring + place * A::kSlot + half * 32 * A::kRowB + k_at;
 #pragma unroll
     for (int k = 0; k < NK; ++k) a[k] = *reinterpret_cast<const bf16x8*>(p + k * 128);
   };
-  auto load_v = [&](bf16x8 (&a)[2], int t, int cb) {
-    const unsigned char* p = slot_of(t) + A::kSlotK + v_at;
+  auto load_v = [&](bf16x8 (&a)[2], int place, int half, int cb) {
+    const unsigned char* p = ring + place * A::kSlot + A::kSlotK + half * 32 * A::kRowB + v_at;
 #pragma unroll
     for (int m = 0; m < 2; ++m) {
       union { s16x4 s[2]; bf16x8 b; } x;
@@ -839,16 +839,14 @@ __global__ __launch_bounds__(512, 2) void paged_chunk_kernel(ChunkParams kp, Pag
 #pragma unroll
     for (int i = 0; i < 16; ++i) acc[cb][i] = 0.f;
   }
-  auto row_of = [&](int t) { return stage_row(t >> 1) + (t & 1) * 32; };
-  auto aux_of = [&](int t, int what) { return aux_all + ((t >> 1) & (A::kDepth - 1)) * A::kAux + what * A::kStage + (t & 1) * 32 + 4 * h; };
-  auto counted = [&](int t) { return cu && row_of(t) < pa.count_pitch; };
-  // some query of the wave does not see some row of the tile, though the row is there
-  auto edge = [&](int t) {
-    const int r = row_of(t);
+  // words of a tile's rows: what 0 logarithms of counts, 1 key scales, 2 value scales
+  auto aux_of = [&](int place, int half, int what) { return aux_all + place * A::kAux + what * A::kStage + half * 32 + 4 * h; };
+  // some query of the wave does not see some row of the 32 from r on, though the row is there
+  auto edge = [&](int r) {
     return (kp.causal && r + 31 > w_lo) || (pa.window > 0 && r <= w_hi - pa.window && r + 32 > pa.sinks);
   };
-  // Bit (i & 3) + 8 (i >> 2): the lane's query sees the row of its element i.
-  auto seen_bits = [&](int t) { return seen_rows(row_of(t), qi, kp.causal, pa.window, pa.sinks) >> (4 * h); };
+  // Bit (i & 3) + 8 (i >> 2): the lane's query sees the row of its element i, of the 32 from r on.
+  auto seen_bits = [&](int r) { return seen_rows(r, qi, kp.causal, pa.window, pa.sinks) >> (4 * h); };
   auto elem_mask = [](uint32_t bits, int i) { return bit_mask(bits, (i & 3) + 8 * (i >> 2)); };
   auto logits = [&](f32x16& o, const bf16x8 (&a)[NK]) {
 #pragma unroll
@@ -862,14 +860,13 @@ __global__ __launch_bounds__(512, 2) void paged_chunk_kernel(ChunkParams kp, Pag
   };
   // A tile that some query does not see whole: values that are not finite out of the product, and marks for those
   // that see one.
-  auto clean = [&](bf16x8 (&a)[2], int t, int cb) {  // (t -1: in front of the first)
+  auto clean = [&](bf16x8 (&a)[2], uint32_t bits, int cb) {  // (bits: seen_bits of the tile; rows that are not there hold zeros)
     uint32_t odd = 0u;
 #pragma unroll
     for (int m = 0; m < 2; ++m)
 #pragma unroll
       for (int e = 0; e < 4; ++e) odd |= not_finite2(__builtin_bit_cast(u32x4, a[m])[e]);
     if (!__any(odd != 0u)) return;
-    const uint32_t bits = t >= 0 ? seen_bits(t) : 0u;  // (rows that are not there hold zeros)
     f32x16 seen;
 #pragma unroll
     for (int i = 0; i < 16; ++i) seen[i] = 0.f;
@@ -893,26 +890,26 @@ __global__ __launch_bounds__(512, 2) void paged_chunk_kernel(ChunkParams kp, Pag
     __builtin_amdgcn_sched_barrier(0);  // (or all blocks' temporaries live at once)
   };
   // Exponents of tile t, in place of its logits ...
-  auto exponents = [&](int t, f32x16& x) {
+  auto exponents = [&](int place, int half, f32x16& x) {
 #pragma unroll
     for (int i4 = 0; i4 < 4; ++i4) {
       f32x4 ck = {c, c, c, c};
-      if constexpr (E4M3) ck = *reinterpret_cast<const f32x4*>(aux_of(t, 1) + 8 * i4);
+      if constexpr (E4M3) ck = *reinterpret_cast<const f32x4*>(aux_of(place, half, 1) + 8 * i4);
 #pragma unroll
       for (int e = 0; e < 4; ++e) x[4 * i4 + e] = __builtin_fmaf(x[4 * i4 + e], ck[e], -ref);
     }
   };
   // ... and where a query does not see every row or a row has a count.
-  auto mask = [&](int t, f32x16& x, uint32_t here) {
-    if (counted(t)) {
+  auto mask = [&](int place, int half, int r, f32x16& x, uint32_t here, bool counted) {
+    if (counted) {
 #pragma unroll
       for (int i4 = 0; i4 < 4; ++i4) {
-        const f32x4 bias = *reinterpret_cast<const f32x4*>(aux_of(t, 0) + 8 * i4);
+        const f32x4 bias = *reinterpret_cast<const f32x4*>(aux_of(place, half, 0) + 8 * i4);
 #pragma unroll
         for (int e = 0; e < 4; ++e) x[4 * i4 + e] += bias[e];
       }
     }
-    const uint32_t bits = seen_bits(t) & (here >> (4 * h));
+    const uint32_t bits = seen_bits(r) & (here >> (4 * h));
 #pragma unroll
     for (int i = 0; i < 16; ++i) x[i] = masked(x[i], elem_mask(bits, i));
   };
@@ -929,19 +926,18 @@ __global__ __launch_bounds__(512, 2) void paged_chunk_kernel(ChunkParams kp, Pag
     return corr;
   };
   auto rescale = [&](float corr) {
-    l *= corr;
 #pragma unroll
     for (int cb = 0; cb < CB; ++cb)
 #pragma unroll
       for (int i = 0; i < 16; ++i) acc[cb][i] *= corr;
   };
   // Weights from exponents, and their sum.
-  auto weights = [&](int t, const f32x16& x, bf16x8 (&w)[2]) {
+  auto weights = [&](int place, int half, const f32x16& x, bf16x8 (&w)[2]) {
     float sum = 0.f;
 #pragma unroll
     for (int i4 = 0; i4 < 4; ++i4) {
       f32x4 vs;
-      if constexpr (E4M3) vs = *reinterpret_cast<const f32x4*>(aux_of(t, 2) + 8 * i4);
+      if constexpr (E4M3) vs = *reinterpret_cast<const f32x4*>(aux_of(place, half, 2) + 8 * i4);
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         float y = __builtin_amdgcn_exp2f(x[4 * i4 + e]);
@@ -975,22 +971,26 @@ __global__ __launch_bounds__(512, 2) void paged_chunk_kernel(ChunkParams kp, Pag
     meet();
     if constexpr (!E4M3) {
       convert_counts(0);
-      if (counted(0)) meet();
+      if (cu) meet();
     }
     bf16x8 a[NK];
-    load_k(a, 0);
+    load_k(a, 0, 0);
     logits(s[0], a);
-    load_k(a, 1);
-    auto flags_of = [&](int s) { return *reinterpret_cast<const u32x2*>(flag_all + (s & (A::kDepth - 1)) * 8); };
+    load_k(a, 0, 1);
+    auto flags_of = [&](int place) { return *reinterpret_cast<const u32x2*>(flag_all + place * 8); };
     u32x2 flag_next = flags_of(0);
     // (Behind the last tile lie zeros; in front of the first, weights of zero meet the first tile's own values.)
-    bool edge_prev = true;
+    int r_prev = -1;             // first row of the tile before
+    bool edge_prev = true, grown_prev = false;
+    float corr = 1.f;
 #pragma unroll
     for (int e = 0; e < 8; ++e) p[1][0][e] = p[1][1][e] = (__bf16)0.f;
     for (int st = 0; st < n_stages; ++st) {
       if (st > 0) meet();
+      const int place = st & (A::kDepth - 1), after = (st + 1) & (A::kDepth - 1), before = st > 0 ? (st - 1) & (A::kDepth - 1) : 0;
+      const int r_stage = stage_row(st);
       const uint32_t here[2] = {(uint32_t)__builtin_amdgcn_readfirstlane((int)flag_next[0]), (uint32_t)__builtin_amdgcn_readfirstlane((int)flag_next[1])};
-      flag_next = flags_of(st + 1);
+      flag_next = flags_of(after);
       if (((st + 3) & 63) == 0) load_entries(st + 3);
       if constexpr (!E4M3) {
         const Place next_k = find(st + 3);
@@ -999,28 +999,34 @@ __global__ __launch_bounds__(512, 2) void paged_chunk_kernel(ChunkParams kp, Pag
         next_v = next_k;
         convert_counts(st + 1);
       }
+      const bool counted = cu && r_stage < pa.count_pitch;
 #pragma unroll
       for (int half = 0; half < 2; ++half) {
-        const int t = 2 * st + half;
-        const bool at_edge = edge(t), special = at_edge || here[half] != ~0u || counted(t);
+        const int r = r_stage + 32 * half;
+        const bool at_edge = edge(r);
         bf16x8 v[CB][2];
 #pragma unroll
-        for (int cb = 0; cb < CB; ++cb) load_v(v[cb], max(t - 1, 0), cb);
+        for (int cb = 0; cb < CB; ++cb) load_v(v[cb], half ? place : before, half ^ (st > 0 || half), cb);
         logits(s[half ^ 1], a);
-        exponents(t, s[half]);
-        if (special) mask(t, s[half], here[half]);
-        float mx = s[half][0], corr = 1.f;
+        exponents(place, half, s[half]);
+        if (at_edge || counted || here[half] != ~0u) mask(place, half, r, s[half], here[half], counted);
+        float mx = s[half][0];
 #pragma unroll
         for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[half][i]);
-        const bool grown = __any(mx > limit) != 0;  // some query's exponents have outgrown its reference, or are its first
-        if (grown) corr = follow(s[half], mx);
-        if (edge_prev)
+        if (edge_prev || grown_prev) {
+          if (grown_prev) rescale(corr);
+          if (edge_prev) {
+            const uint32_t bits = r_prev < 0 ? 0u : seen_bits(r_prev);
 #pragma unroll
-          for (int cb = 0; cb < CB; ++cb) clean(v[cb], t - 1, cb);
-        load_k(a, t + 2);
+            for (int cb = 0; cb < CB; ++cb) clean(v[cb], bits, cb);
+          }
+        }
+        grown_prev = __any(mx > limit) != 0;  // some query's exponents have outgrown its reference, or are its first:
+        if (grown_prev) corr = follow(s[half], mx);  // its sums follow when this tile's values join them
+        load_k(a, after, half);
 #pragma unroll
         for (int cb = 0; cb < CB; ++cb) values(v[cb], p[half ^ 1], cb);
-        float ps = weights(t, s[half], p[half]);
+        float ps = weights(place, half, s[half], p[half]);
         asm volatile("" : "+v"(ps));  // (or the weights move behind the branch below, away from the products they run beside)
 #pragma unroll
         for (int k = 0; k < 2 * CB; ++k) {
@@ -1029,9 +1035,9 @@ __global__ __launch_bounds__(512, 2) void paged_chunk_kernel(ChunkParams kp, Pag
           __builtin_amdgcn_sched_group_barrier(0x400, 16 / (2 * CB), 0);  // exponentials
           __builtin_amdgcn_sched_group_barrier(0x002, 24 / (2 * CB) + 1, 0);
         }
-        if (grown) rescale(corr);
-        l += ps;
+        l = __builtin_fmaf(l, grown_prev ? corr : 1.f, ps);
         edge_prev = at_edge;
+        r_prev = r;
         if constexpr (E4M3)
           if (half == 0) {
             commit(st + 2);
@@ -1039,12 +1045,12 @@ __global__ __launch_bounds__(512, 2) void paged_chunk_kernel(ChunkParams kp, Pag
           }
       }
     }
-    const int last = 2 * n_stages - 1;
+    if (grown_prev) rescale(corr);
 #pragma unroll
     for (int cb = 0; cb < CB; ++cb) {
       bf16x8 v[2];
-      load_v(v, last, cb);
-      if (edge_prev) clean(v, last, cb);
+      load_v(v, (n_stages - 1) & (A::kDepth - 1), 1, cb);
+      if (edge_prev) clean(v, seen_bits(r_prev), cb);
       values(v, p[1], cb);
     }
 #pragma unroll
