@@ -568,9 +568,11 @@ int cask_attend_paged(const cask_params* params, const cask_pages* pages, const 
   pa.window = window;
   pa.sinks = sinks;
   pa.part = static_cast<float*>(ws);
-  pa.splits = ws ? paged_splits(kp, pa.pg.n_units, pa.rw.max_n, e4m3, window, sinks, paged_max_rows(pa.pg, max_rows)) : 1;
+  const int most = paged_max_rows(pa.pg, max_rows);
+  const PagedPlan plan = paged_plan(kp, pa.pg.n_units, pa.rw.max_n, e4m3, window, sinks, most);
+  pa.splits = ws ? plan.splits : 1;
   if (paged_part_bytes(kp, pa.pg.n_units, pa.rw.max_n, pa.splits) > ws_bytes) pa.splits = 1;
-  return dev_rc(launch_attend_paged(kp, pa, e4m3, paged_max_rows(pa.pg, max_rows), static_cast<hipStream_t>(hip_stream)));
+  return dev_rc(launch_attend_paged(kp, pa, plan.chunk, e4m3, most, static_cast<hipStream_t>(hip_stream)));
 }
 
 size_t cask_attend_paged_workspace_bytes(const cask_params* params, const cask_pages* pages, const cask_rows* rows,
@@ -582,7 +584,7 @@ size_t cask_attend_paged_workspace_bytes(const cask_params* params, const cask_p
   if (resolve_paged(params, pages, rows, &kp, &pg, &rw, false, &none) != CASK_OK || none) return 0;
   if (window < 0 || sinks < 0 || max_rows < 0) return 0;
   return paged_part_bytes(kp, pg.n_units, rw.max_n,
-                          paged_splits(kp, pg.n_units, rw.max_n, pages->type == CASK_E4M3, window, sinks, paged_max_rows(pg, max_rows)));
+                          paged_plan(kp, pg.n_units, rw.max_n, pages->type == CASK_E4M3, window, sinks, paged_max_rows(pg, max_rows)).splits);
 }
 
 int cask_compress(const cask_params* params, const cask_batch* batch, void* K_out, void* V_out,

@@ -424,9 +424,13 @@ struct PagedAttend {
   int splits;         // workgroups that share the rows of a block of queries
   float* part;        // their partial results
 };
-// Splits of such a call (max_rows: about the largest number of rows a unit holds) and the bytes of their results.
-int paged_splits(const KParams& kp, int n_units, int max_n, bool e4m3, int window, int sinks, int max_rows);
+// How such a call is done (max_rows: about the largest number of rows a unit holds), and the bytes of its splits' results.
+struct PagedPlan {
+  bool chunk;  // blocks of 256 query rows, else of 16 or 32
+  int splits;
+};
+PagedPlan paged_plan(const KParams& kp, int n_units, int max_n, bool e4m3, int window, int sinks, int max_rows);
 size_t paged_part_bytes(const KParams& kp, int n_units, int max_n, int splits);
-hipError_t launch_attend_paged(const KParams& kp, const PagedAttend& pa, bool e4m3, int max_rows, hipStream_t st);
+hipError_t launch_attend_paged(const KParams& kp, const PagedAttend& pa, bool chunk, bool e4m3, int max_rows, hipStream_t st);
 
 }  // namespace cask

@@ -562,12 +562,56 @@ __global__ __launch_bounds__(WAVES * 64, 8 / WAVES) void paged_rows_kernel(KPara
   }
 }
 
-// Adds the splits of a query row: a wave finds their common reference, a workgroup's 256 / (D / 4) groups of threads
-// take every so many-th of them, the groups' sums are added in order.  (A thread per channel that goes through the
-// splits one by one: 28 rows of 64 splits 20 us.)
+constexpr int kMostSplits = 64, kFewSplits = 8;
+
+// Adds the splits of a query row under their common reference, in their order.
+// FEW: D / 4 threads a row, which hold all of its splits at once (28 672 rows of 2 splits: a workgroup each 40 us).
+template <typename T, int D>
+__global__ __launch_bounds__(256) void paged_combine_few_kernel(int G, PagedAttend pa, int64_t rows) {
+  constexpr int kLanes = D / 4;
+  const int64_t o = (int64_t)blockIdx.x * (256 / kLanes) + threadIdx.x / kLanes, per_unit = (int64_t)pa.rw.max_n * G;
+  if (o >= rows) return;
+  const int ch = (threadIdx.x % kLanes) * 4, S = pa.splits;
+  const int u = (int)(o / per_unit), m = (int)(o % per_unit);
+  if (m >= rows_of_unit(pa.rw, u) * G) return;
+  const int64_t row = array_row(pa.rw, first_of_unit(pa.rw, u), m / G);
+  if (row < 0) return;
+  f32x2 st[kFewSplits];
+  f32x4 v[kFewSplits];
+  float top = kNegInf;
+#pragma unroll
+  for (int i = 0; i < kFewSplits; ++i) {
+    st[i] = i < S ? part_state(pa, G, D)[o * S + i] : f32x2{kNegInf, 0.f};
+    v[i] = i < S ? *reinterpret_cast<const f32x4*>(pa.part + (o * S + i) * D + ch) : f32x4{0.f, 0.f, 0.f, 0.f};
+    top = fmaxf(top, st[i][0]);
+  }
+  f32x4 num = {0.f, 0.f, 0.f, 0.f};
+  float den = 0.f;
+#pragma unroll
+  for (int i = 0; i < kFewSplits; ++i)
+    if (i < S) {
+      const float f = share(st[i][0], top);
+      num += v[i] * f;
+      den = __builtin_fmaf(st[i][1], f, den);
+    }
+  T* out = static_cast<T*>(pa.out) + (row * G + m % G) * D + ch;
+  if constexpr (sizeof(T) == 4) {
+    *reinterpret_cast<f32x4*>(out) = f32x4{joined(num[0], den), joined(num[1], den), joined(num[2], den), joined(num[3], den)};
+  } else {
+    u32x2 w;
+#pragma unroll
+    for (int e = 0; e < 2; ++e)
+      w[e] = (uint32_t)float_to_bf16_bits(joined(num[2 * e], den)) | (uint32_t)float_to_bf16_bits(joined(num[2 * e + 1], den)) << 16;
+    *reinterpret_cast<u32x2*>(out) = w;
+  }
+}
+
+// Many splits: a wave finds the reference, a workgroup's 256 / (D / 4) groups of threads take every so many-th split,
+// the groups' sums are added in order.  (A thread per channel that goes through the splits one by one: 28 rows of 64
+// splits 20 us, this 4.)
 template <typename T, int D>
 __global__ __launch_bounds__(256) void paged_combine_kernel(int G, PagedAttend pa) {
-  constexpr int kLanes = D / 4, kGroups = 256 / kLanes, kMost = 64;  // (kMost: paged_splits)
+  constexpr int kLanes = D / 4, kGroups = 256 / kLanes, kMost = kMostSplits;
   __shared__ float factor[kMost];
   __shared__ float total;
   __shared__ __align__(16) float sums[kGroups][D];
@@ -1147,39 +1191,63 @@ hipError_t launch_rows(const KParams& kp, const PagedAttend& pa, int64_t bytes, 
 
 template <typename T, int D>
 hipError_t launch_combine(const KParams& kp, const PagedAttend& pa, hipStream_t st) {
-  if (pa.splits > 1) paged_combine_kernel<T, D><<<dim3((unsigned)((int64_t)pa.pg.n_units * pa.rw.max_n * kp.G)), dim3(256), 0, st>>>(kp.G, pa);
+  const int64_t rows = (int64_t)pa.pg.n_units * pa.rw.max_n * kp.G;
+  constexpr int kRows = 256 / (D / 4);
+  if (pa.splits > kFewSplits) paged_combine_kernel<T, D><<<dim3((unsigned)rows), dim3(256), 0, st>>>(kp.G, pa);
+  else if (pa.splits > 1)
+    paged_combine_few_kernel<T, D><<<dim3((unsigned)((rows + kRows - 1) / kRows)), dim3(256), 0, st>>>(kp.G, pa, rows);
   return hipGetLastError();
 }
 
-bool chunk_fits(const KParams& kp, int max_n) { return kp.dtype == CASK_BF16 && (int64_t)max_n * kp.G > 64; }
-
 }  // namespace
 
-int paged_splits(const KParams& kp, int n_units, int max_n, bool e4m3, int window, int sinks, int max_rows) {
-  (void)e4m3;
-  const bool chunk = chunk_fits(kp, max_n);
-  const int64_t per_block = chunk ? ChunkGeom<128>::kBlockQ : (kp.dtype == CASK_BF16 || kp.d == 64) && (int64_t)max_n * kp.G > kCols ? 2 * kCols : kCols;
-  const int64_t blocks = (int64_t)n_units * (((int64_t)max_n * kp.G + per_block - 1) / per_block);
-  int64_t rows = max_rows;
-  if (window > 0) rows = rows < (int64_t)window + max_n + sinks ? rows : (int64_t)window + max_n + sinks;
-  const int tile = chunk ? 64 : (kp.dtype == CASK_BF16 ? 32 : 16) * 8;
-  const int rounds = (int)((rows + tile - 1) / tile);
-  if (blocks > 128 || rounds < 4) return 1;
-  int s = (int)(256 / blocks);
-  if (s > rounds / 2) s = rounds / 2;
-  return s > 64 ? 64 : (s < 1 ? 1 : s);
+// Which kernel, and how many workgroups share the rows of a block of queries.  By what a call takes, as measured (us):
+// rounds of the 256 compute units, each `start` + `row` for every row that a workgroup goes through; with splits 4 for
+// the launch that adds them and their results' way to memory and back at 4 TB/s.
+//   form                       start   us per 1000 rows, 128 / 64 channels
+//   up to 16 query rows          4       9 / 5      (4 units of 32 768 rows 15 in all; 512 of 2100 52)
+//   up to 32                     4      15.5 / 9    (64 units of 4000 rows, 64 query rows 41; 256 of 1500 55)
+//   the same, fp32               4      32 / 32
+//   256, bf16 / e4m3             6      36 / 45, 23 / 27
+// The form of 256 query rows is slower per row of the cache and takes eight times as many queries along: 4 units of
+// 30 000 rows with 128 / 192 / 256 query rows each 38 / 47 / 53 by 32, 35 / 37 / 40 by 256; 64 of 500 19 / 34 / 36 and
+// 33 / 38 / 44; 256 of 1500 with 64 / 96 / 128 55 / 78 / 101 and 55 / 56 / 57.
+PagedPlan paged_plan(const KParams& kp, int n_units, int max_n, bool e4m3, int window, int sinks, int max_rows) {
+  const int64_t m = (int64_t)max_n * kp.G;
+  const bool f32 = kp.dtype == CASK_F32, wide = kp.d == 128;
+  auto cost = [&](int64_t block, int least, double start, double per_row, int* splits) {
+    const int64_t blocks = (int64_t)n_units * ((m + block - 1) / block);
+    int64_t rows = max_rows;
+    const int64_t tokens = (block < m ? block : m) / kp.G + 1;
+    if (window > 0 && window + tokens + sinks < rows) rows = window + tokens + sinks;
+    double best = 0.0;
+    for (int s = 1; s <= kMostSplits && (s == 1 || rows >= (int64_t)s * least); ++s) {
+      // (a split's launch counts workgroups in 31 bits, the one behind it query rows)
+      if (s > 1 && (blocks * s > (1 << 28) || n_units * m > (1 << 28))) break;
+      double c = (double)((blocks * s + 255) / 256) * (start + per_row * 1e-3 * (double)((rows + s - 1) / s));
+      if (s > 1) c += 4.0 + (double)n_units * m * s * kp.d * 8.0 / 4.0e6;
+      if (s == 1 || c < best) best = c, *splits = s;
+    }
+    return best;
+  };
+  PagedPlan few{false, 1}, many{true, 1};
+  const bool two = m > kCols && (!f32 || !wide);
+  const double c_few = cost(two ? 2 * kCols : kCols, 256, 4.0, f32 ? 32.0 : two ? (wide ? 15.5 : 9.0) : (wide ? 9.0 : 5.0), &few.splits);
+  if (f32 || m <= 2 * kCols) return few;
+  const double c_many = cost(ChunkGeom<128>::kBlockQ, 128, 6.0, wide ? (e4m3 ? 45.0 : 36.0) : (e4m3 ? 27.0 : 23.0), &many.splits);
+  return c_many < c_few ? many : few;
 }
 
 size_t paged_part_bytes(const KParams& kp, int n_units, int max_n, int splits) {
   return splits <= 1 ? 0 : (size_t)n_units * max_n * kp.G * splits * (kp.d + 2) * sizeof(float);
 }
 
-hipError_t launch_attend_paged(const KParams& kp, const PagedAttend& pa, bool e4m3, int max_rows, hipStream_t st) {
+hipError_t launch_attend_paged(const KParams& kp, const PagedAttend& pa, bool chunk, bool e4m3, int max_rows, hipStream_t st) {
   int64_t rows = max_rows;  // what a unit's queries see, at the most
   if (pa.window > 0 && (int64_t)pa.window + pa.rw.max_n + pa.sinks < rows) rows = (int64_t)pa.window + pa.rw.max_n + pa.sinks;
   const int64_t bytes = pa.pg.n_units * rows * 2 * kp.d * (e4m3 ? 1 : kp.dtype == CASK_F32 ? 4 : 2);
   hipError_t e;
-  if (chunk_fits(kp, pa.rw.max_n)) {
+  if (chunk) {
     if (kp.d == 64) e = e4m3 ? launch_chunk<true, 64>(kp, pa, st) : launch_chunk<false, 64>(kp, pa, st);
     else e = e4m3 ? launch_chunk<true, 128>(kp, pa, st) : launch_chunk<false, 128>(kp, pa, st);
   } else {
