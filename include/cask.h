@@ -125,7 +125,9 @@ enum {
   CASK_PATH_NO_FUSED_SWEEPS = 16, /* many long units with W*G <= 512: two scoring launches instead of one */
   CASK_PATH_FORCE_FUSED_SWEEPS = 32, /* W*G <= 512: one scoring launch whatever the number of units */
   CASK_PATH_NARROW_ROWS = 64, /* both scoring sweeps: 64 resident rows per wave (256 per workgroup) whatever the shape */
-  CASK_PATH_WIDE_ROWS = 128   /* both scoring sweeps: 128 resident rows per wave (512 per workgroup) whatever the shape */
+  CASK_PATH_WIDE_ROWS = 128,  /* both scoring sweeps: 128 resident rows per wave (512 per workgroup) whatever the shape */
+  CASK_PATH_PAGED_FEW = 256,  /* cask_attend_paged: blocks of 16 or 32 query rows whatever the shape */
+  CASK_PATH_PAGED_MANY = 512  /* cask_attend_paged, bf16: blocks of 256 query rows whatever the shape */
 };
 
 typedef struct {

@@ -26,6 +26,7 @@ PATH_NO_FUSED_TAIL, PATH_NO_FUSED_SCORE, PATH_DEDUP_VECTOR, PATH_ATTEND_VECTOR, 
 PATH_FORCE_FUSED_SWEEPS = 32
 PATH_NARROW_ROWS = 64
 PATH_WIDE_ROWS = 128
+PATH_PAGED_FEW, PATH_PAGED_MANY = 256, 512
 (ROLE_PREFIX_DROP, ROLE_PREFIX_KEEP, ROLE_CORE, ROLE_SEED, ROLE_DONOR, ROLE_RECENT,
  ROLE_DECODE_EVICT) = range(7)
 
@@ -447,12 +448,8 @@ def attend(p: Params, Q: torch.Tensor, K_c: torch.Tensor, V_c: torch.Tensor, len
 _ROW_DTYPES = {torch.float32: F32, torch.bfloat16: BF16, torch.float8_e4m3fn: E4M3}
 
 
-def _on(device: torch.device, *tensors) -> None:
-    """All of them on `device`, which is the current one: the stream a call goes to is the current device's."""
-    for t in tensors:
-        assert t is None or t.device == device, (t.device, device)
-    current = _raw_device() if _raw_device is not None else torch.cuda.current_device()
-    assert device.type == "cuda" and device.index == current, f"tensors on {device}, current device {current}"
+def _current_device() -> int:
+    return _raw_device() if _raw_device is not None else torch.cuda.current_device()
 
 
 class Pages:
@@ -484,7 +481,8 @@ class Pages:
         for t in (K, V, K_scale, V_scale, table):
             assert t is None or (t.is_cuda and t.device == K.device), "device-resident tensors expected"
         self.params, self.K, self.V, self.K_scale, self.V_scale, self.table = p, K, V, K_scale, V_scale, table
-        self.device = K.device
+        self.device, self._index = K.device, K.device.index
+        self._rows_dtype = torch.float32 if p.dtype == F32 else torch.bfloat16   # of the arrays that calls bring
         self.n_units = n_pages if table is None else table.shape[0]
         ptr = [None if t is None else t.data_ptr() for t in (table, K, V, K_scale, V_scale)]
         self._c = _Pages(kind, self.n_units, n_pages, page_rows, pitch, 0 if table is None else table.shape[1], *ptr)
@@ -515,21 +513,24 @@ class Rows:
         for t, dt in ((start, torch.int32), (first, torch.int64)):
             assert t is None or (t.dtype == dt and t.shape == n.shape and t.device == n.device and t.is_contiguous())
         self.n, self.start, self.first, self.max_n, self.pitch = n, start, first, int(max_n), int(pitch)
+        self.device = n.device
         self._ptr = [None if t is None else t.data_ptr() for t in (n, start, first)]
 
     def c(self, total: int) -> _Rows:
         return _Rows(self.max_n, self.pitch, total, *self._ptr)
 
 
-def _paged_arrays(pages: Pages, rows: Rows, per_row: int, *arrays) -> int:
-    """Rows of the call's arrays, `per_row` elements each, after the checks that all paged calls share."""
-    want = torch.float32 if pages.params.dtype == F32 else torch.bfloat16
-    for t in arrays:
-        assert t.dtype == want and t.is_contiguous() and t.shape == arrays[0].shape, (t.dtype, want, t.shape)
-        assert t.shape[-1] == pages.params.head_dim and t.numel() % per_row == 0
+def _paged_arrays(pages: Pages, rows: Rows, per_row: int, x: torch.Tensor, y: torch.Tensor) -> int:
+    """Rows of a call's two arrays, `per_row` elements each, after the checks that all paged calls share.  Everything lies
+    on the current device: the stream a call goes to is that device's."""
+    want, dev, n = pages._rows_dtype, pages.device, x.numel()
+    assert x.dtype == want and y.dtype == want, (x.dtype, y.dtype, want)
+    assert x.shape == y.shape and x.shape[-1] == pages.params.head_dim and n % per_row == 0, (x.shape, y.shape)
+    assert x.is_contiguous() and y.is_contiguous()
     assert rows.n.numel() == pages.n_units, (rows.n.numel(), pages.n_units)
-    _on(pages.device, rows.n, *arrays)
-    return arrays[0].numel() // per_row
+    assert x.device == dev and y.device == dev and rows.device == dev, (x.device, y.device, rows.device, dev)
+    assert pages._index == _current_device(), f"tensors on {dev}, current device {_current_device()}"
+    return n // per_row
 
 
 def cache_write(pages: Pages, rows: Rows, K: torch.Tensor, V: torch.Tensor) -> None:

@@ -1233,9 +1233,10 @@ PagedPlan paged_plan(const KParams& kp, int n_units, int max_n, bool e4m3, int w
   PagedPlan few{false, 1}, many{true, 1};
   const bool two = m > kCols && (!f32 || !wide);
   const double c_few = cost(two ? 2 * kCols : kCols, 256, 4.0, f32 ? 32.0 : two ? (wide ? 15.5 : 9.0) : (wide ? 9.0 : 5.0), &few.splits);
-  if (f32 || m <= 2 * kCols) return few;
+  const bool ask_many = (kp.path_flags & CASK_PATH_PAGED_MANY) != 0, ask_few = (kp.path_flags & CASK_PATH_PAGED_FEW) != 0;
+  if (f32 || ask_few || (m <= 2 * kCols && !ask_many)) return few;
   const double c_many = cost(ChunkGeom<128>::kBlockQ, 128, 6.0, wide ? (e4m3 ? 45.0 : 36.0) : (e4m3 ? 27.0 : 23.0), &many.splits);
-  return c_many < c_few ? many : few;
+  return c_many < c_few || ask_many ? many : few;
 }
 
 size_t paged_part_bytes(const KParams& kp, int n_units, int max_n, int splits) {

@@ -186,14 +186,21 @@ def test_one_token(dtype, cache, d, G, page_rows):
         _attend(pages, n, start, first, 1, len(lens), seed=G, **kw)
 
 
+FORMS = [0, B.PATH_PAGED_FEW, B.PATH_PAGED_MANY]   # the library's choice, blocks of few query rows, blocks of many
+
+
+@pytest.mark.parametrize("form", FORMS)
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("dtype,cache", TYPES)
 @pytest.mark.parametrize("G,page_rows", [(1, 64), (4, 16), (7, 32)])
-def test_chunks(dtype, cache, d, G, page_rows):
+def test_chunks(dtype, cache, d, G, page_rows, form):
     """Chunks of different length (none, one token, odd numbers, hundreds) behind caches of different length, in token
     order with several heads; causal, not causal, windows narrower and wider than chunk and tile."""
+    if dtype == "f32" and form == B.PATH_PAGED_MANY:
+        pytest.skip("blocks of many query rows are bf16's")
     heads, new, past = 2, [1, 0, 37, 130, 300], [50, 3, 0, 77, 500]
-    pages = plain.make(dtype, cache, d, G, units=heads * len(new), page_rows=page_rows, cap_pages=-(-800 // page_rows), seed=G + d)
+    pages = plain.make(dtype, cache, d, G, units=heads * len(new), page_rows=page_rows, cap_pages=-(-800 // page_rows), seed=G + d,
+                       params_kw=dict(path_flags=form))
     begin = [sum(new[:i]) for i in range(len(new))]
     n, start = [x for x in new for _ in range(heads)], [x for x in past for _ in range(heads)]
     first = [b * heads + h for b in begin for h in range(heads)]
@@ -201,20 +208,24 @@ def test_chunks(dtype, cache, d, G, page_rows):
     for kw in (dict(), dict(count=count), dict(window=33, sinks=4), dict(window=200, sinks=17, count=count), dict(window=1)):
         _attend(pages, n, start, first, heads, sum(new) * heads, seed=G, **kw)
     loose = plain.make(dtype, cache, d, G, units=heads * len(new), page_rows=page_rows, cap_pages=-(-800 // page_rows), seed=G + d,
-                       params_kw=dict(causal=0))
+                       params_kw=dict(causal=0, path_flags=form))
     _attend(loose, n, start, first, heads, sum(new) * heads, seed=G, causal=False)
     _attend(loose, n, start, first, heads, sum(new) * heads, seed=G, causal=False, window=50, sinks=2)
 
 
+@pytest.mark.parametrize("form", FORMS)
 @pytest.mark.parametrize("dtype,cache", TYPES)
-def test_few_units_many_rows_share_the_work(dtype, cache):
+def test_few_units_many_rows_share_the_work(dtype, cache, form):
     """One unit of thousands of rows, one token and a short chunk: the splits' results together, and with no workspace
     or one a byte too small, a single workgroup's; the capacity in place of the rows' number gives the same."""
+    if dtype == "f32" and form == B.PATH_PAGED_MANY:
+        pytest.skip("blocks of many query rows are bf16's")
     for n, past in (([1], [5000]), ([9], [4001]), ([40], [6000])):
-        pages = plain.make(dtype, cache, 128, 4, units=1, page_rows=64, cap_pages=96, seed=n[0])
+        pages = plain.make(dtype, cache, 128, 4, units=1, page_rows=64, cap_pages=96, seed=n[0], params_kw=dict(path_flags=form))
         p = pages.params
-        _attend(pages, n, past, [0], 1, n[0], max_rows=past[0] + n[0])
-        _attend(pages, n, past, [0], 1, n[0])
+        one = n[0] == 1 and form != B.PATH_PAGED_MANY
+        _attend(pages, n, past, [0], 1, n[0], max_rows=past[0] + n[0], one=one)
+        _attend(pages, n, past, [0], 1, n[0], one=one)
         lib, r = cask.load(), plain.rows(n, past, [0])
         Q = torch.randn(n[0], 4, 128, generator=torch.Generator().manual_seed(0)).to(plain.TORCH[dtype])
         outs = [torch.zeros_like(Q).cuda() for _ in range(3)]
@@ -228,21 +239,24 @@ def test_few_units_many_rows_share_the_work(dtype, cache):
         torch.cuda.synchronize()
         want = plain.attend(plain.host(pages), Q, n, past, [0], 1)
         for o in outs:
-            plain.check_attend(o, want, dtype, n[0] == 1)
+            plain.check_attend(o, want, dtype, n[0] == 1 and form != B.PATH_PAGED_MANY)
         assert _same(outs[0], outs[1])
         assert _same(outs[2], cask.attend_paged(pages, r, Qd))
 
 
+@pytest.mark.parametrize("form", FORMS)
 @pytest.mark.parametrize("dtype,cache", TYPES)
 @pytest.mark.parametrize("n", [1, 60])
-def test_rows_that_are_not_seen_may_hold_anything(dtype, cache, n):
+def test_rows_that_are_not_seen_may_hold_anything(dtype, cache, n, form):
     """NaN and infinities in rows behind the unit's last, in front of a window, behind a query, in the scales of pages
     and in pages of nobody: queries that do not see them give the same bits as over clean rows.  Queries that do
     see them get what they hold."""
+    if dtype == "f32" and form == B.PATH_PAGED_MANY:
+        pytest.skip("blocks of many query rows are bf16's")
     past, window, sinks = 200, 12, 3
     bad_rows = [5, 40, past - 20, past + 7, past + 30, past + n, past + n + 1]
-    pages = plain.make(dtype, cache, 128, 4, units=2, page_rows=32, cap_pages=12, seed=4)
-    clean = plain.make(dtype, cache, 128, 4, units=2, page_rows=32, cap_pages=12, seed=4)
+    pages = plain.make(dtype, cache, 128, 4, units=2, page_rows=32, cap_pages=12, seed=4, params_kw=dict(path_flags=form))
+    clean = plain.make(dtype, cache, 128, 4, units=2, page_rows=32, cap_pages=12, seed=4, params_kw=dict(path_flags=form))
     used = set(int(e) for e in pages.table.flatten())
     for c, fill in ((pages, float("nan")),):
         for pool in (c.K, c.V):
@@ -277,8 +291,8 @@ def test_rows_that_are_not_seen_may_hold_anything(dtype, cache, n):
 
 def test_values_that_are_not_finite_reach_those_who_see_them():
     """A value that is not finite in one channel: not finite for the queries behind it, in that channel alone."""
-    for dtype in ("bf16", "f32"):
-        pages = plain.make(dtype, dtype, 64, 2, units=1, page_rows=16, cap_pages=8, seed=2)
+    for dtype, form in (("bf16", 0), ("f32", 0), ("bf16", B.PATH_PAGED_MANY)):
+        pages = plain.make(dtype, dtype, 64, 2, units=1, page_rows=16, cap_pages=8, seed=2, params_kw=dict(path_flags=form))
         for row, ch, x in ((10, 3, float("inf")), (20, 5, -float("inf")), (35, 60, float("nan"))):
             e, w = plain.place(plain.host(pages), 0, row)
             pages.V[e, w, ch] = x
@@ -291,8 +305,8 @@ def test_values_that_are_not_finite_reach_those_who_see_them():
 
 def test_a_row_that_sees_nothing_is_zero():
     """Pages that are not there, a start in front of the cache, a start behind its capacity."""
-    for dtype, cache in TYPES:
-        pages = plain.make(dtype, cache, 128, 3, units=4, page_rows=16, cap_pages=6, seed=1)
+    for dtype, cache, form in [(*t, 0) for t in TYPES] + [("bf16", "bf16", B.PATH_PAGED_MANY), ("bf16", "e4m3", B.PATH_PAGED_MANY)]:
+        pages = plain.make(dtype, cache, 128, 3, units=4, page_rows=16, cap_pages=6, seed=1, params_kw=dict(path_flags=form))
         pages.table[0] = -1
         pages.table[1, 1:] = 1 << 30
         n, start = [20, 30, 30, 10], [10, 5, -12, 96]
@@ -301,12 +315,13 @@ def test_a_row_that_sees_nothing_is_zero():
         assert (out[:20] == 0).all() and (out[20 + 21: 50] == 0).all() and (out[50:62] == 0).all()
         _attend(pages, n, start, first, 1, 90)
         one = [1, 1, 1, 1]
-        _attend(pages, one, [3, 30, -1, 200], [0, 1, 2, 3], 1, 4, window=4)
+        _attend(pages, one, [3, 30, -1, 200], [0, 1, 2, 3], 1, 4, window=4, one=not form)
 
 
-def test_bounds_of_a_call():
+@pytest.mark.parametrize("form", FORMS)
+def test_bounds_of_a_call(form):
     """n above max_n counts as max_n, a negative one as none; rows outside the arrays are neither read nor written."""
-    pages = plain.make("bf16", "e4m3", 64, 2, units=4, page_rows=16, cap_pages=20, seed=8)
+    pages = plain.make("bf16", "e4m3", 64, 2, units=4, page_rows=16, cap_pages=20, seed=8, params_kw=dict(path_flags=form))
     Q = torch.randn(100, 2, 64, generator=torch.Generator().manual_seed(0)).to(torch.bfloat16)
     for dev_n, n, first in (([50, -4, 12, 30], [20, 0, 12, 20], [0, 10, 95, -3]), ([1 << 30, 1, 7, 9], [20, 1, 7, 9], [60, 99, 100, 1 << 45])):
         start = [9, 100, 31, 250]
@@ -360,6 +375,38 @@ def test_same_bits_every_run_and_on_another_stream():
             got = cask.attend_paged(pages, r, Q)
         side.synchronize()
         assert _same(got, want) and _same(cask.attend_paged(pages, r, Q), want)
+
+
+@pytest.mark.parametrize("cache", ["bf16", "e4m3"])
+def test_long_caches_in_blocks_of_many_query_rows(cache):
+    """More than 64 stages of 64 rows (the pages are looked up 64 at a time), counts that end in the middle of a stage,
+    missing pages, a window that leaves a gap behind the first rows; few of the queries are compared."""
+    past, n = 8500, 33
+    pages = plain.make("bf16", cache, 64, 1, units=1, page_rows=16, cap_pages=540, seed=12, params_kw=dict(path_flags=B.PATH_PAGED_MANY))
+    for e in (3, 77, 130, 262, 400, 401, 402, 403, 404):
+        pages.table[0, e] = -1
+    count = torch.randint(1, 5, (1, 4811), generator=torch.Generator().manual_seed(3), dtype=torch.int32)
+    for kw in (dict(), dict(count=count), dict(window=5000, sinks=130, count=count), dict(window=64 * 64 + 5, sinks=1)):
+        _attend(pages, [n], [past], [0], 1, n, one=False, **kw)
+
+
+def test_references_that_have_to_follow():
+    """Logits that grow by hundreds along the cache, and fall by as many: every sum is rescaled again and again, and what
+    came before keeps its weight where that does not vanish."""
+    for form in (B.PATH_PAGED_FEW, B.PATH_PAGED_MANY):
+        for sign in (1.0, -1.0):
+            pages = plain.make("bf16", "bf16", 64, 2, units=1, page_rows=16, cap_pages=20, seed=3, params_kw=dict(path_flags=form))
+            ramp = sign * torch.linspace(-40, 40, 320)
+            e = pages.table[0].long().cpu()
+            K = pages.K.cpu().float()
+            K[e, :, 0] = ramp.view(20, 16)
+            pages.K.copy_(K.to(torch.bfloat16))
+            Q = torch.randn(40, 2, 64, generator=torch.Generator().manual_seed(0))
+            Q[..., 0] = 60.0
+            Q = Q.to(torch.bfloat16)
+            out = cask.attend_paged(pages, plain.rows([40], [280]), Q.cuda())
+            torch.cuda.synchronize()
+            plain.check_attend(out, plain.attend(plain.host(pages), Q, [40], [280], [0], 1), "bf16", False)
 
 
 # ---------------------------------------------------------------- together
