@@ -332,10 +332,10 @@ typedef struct {
   int32_t type;        /* CASK_E4M3, or params->dtype */
   int32_t n_units;
   int32_t n_pages;     /* pages of the pools (without a table >= n_units) */
-  int32_t page_rows;   /* a power of two, 16 to 2^20; without a table any number >= 1 (CASK_E4M3: of 16s) */
+  int32_t page_rows;   /* a power of two, 16 to 2^20; without a table 1 to 2^29 (CASK_E4M3: a multiple of 16) */
   int64_t page_pitch;  /* pool rows from the start of a page to that of the next, >= page_rows; a row has d
                           elements in K and V, one in the scales */
-  int32_t table_pitch; /* entries per unit, table_pitch * page_rows <= 2^30 */
+  int32_t table_pitch; /* entries per unit, table_pitch * page_rows <= 2^29 */
   const int32_t* table; /* DEVICE [n_units, table_pitch] or NULL */
   void* K;             /* DEVICE, 16-byte aligned: pool of keys, row 0 of page 0 */
   void* V;             /* DEVICE, 16-byte aligned */
@@ -348,11 +348,11 @@ typedef struct {
  * sequences back to back: first = tokens before the sequence * heads + head, pitch = heads; arrays [n_units, max_n,
  * ...]: first NULL, pitch 1. */
 typedef struct {
-  int32_t max_n;        /* HOST: n[u] is taken as at most this; sizes the launch */
+  int32_t max_n;        /* HOST: n[u] is taken as at most this; sizes the launch.  max_n * G <= 2^29, n_units * max_n < 2^31 */
   int64_t pitch;        /* >= 1 */
   int64_t total;        /* rows of the call's arrays: rows outside [0, total) are neither read nor written */
   const int32_t* n;     /* DEVICE [n_units]; a negative one counts as 0 */
-  const int32_t* start; /* DEVICE [n_units] or NULL: 0 */
+  const int32_t* start; /* DEVICE [n_units] or NULL: 0.  -2^30 to 2^30 */
   const int64_t* first; /* DEVICE [n_units] or NULL: u * max_n */
 } cask_rows;
 
@@ -376,6 +376,8 @@ int cask_cache_read(const cask_params* params, const cask_pages* pages, const ca
  *   count [n_units, count_pitch] DEVICE or NULL, as in cask_attend: the tokens a row stands for (< 1 and rows at or
  *         behind count_pitch: 1)
  *   window, sinks  >= 0; window 0: every row; sinks are used with a window only
+ *   (n_units * max_n * G up to 2^26 in float32, 2^30 in bfloat16: CASK_EINVAL where that takes more than 2^22 blocks of
+ *   16, of 256 query rows)
  *   max_rows  HOST: about the largest start + n of the units, 0 = the capacity; only a choice of how the work is
  *         dealt out goes by it (the same value gives the same bits)
  *   ws    DEVICE, 16-byte aligned: where few queries see many rows, several workgroups share them and leave partial

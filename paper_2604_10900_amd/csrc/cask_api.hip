@@ -269,6 +269,10 @@ struct StageRecorder {
 // The host side of a paged cache and of a call's rows: checked, and as the kernels take them.
 static bool misaligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) != 0; }
 
+// Rows of a unit, and query rows of one: with places held to +-2^30 (a start further out has its rows outside every
+// capacity) and windows to 2^30, no sum or difference of these leaves 32 bits.
+constexpr int kMostUnitRows = 1 << 29;
+
 // `pointers`: the device pointers are checked as well (not where only sizes are asked for).
 static int resolve_pages(const KParams& kp, const cask_pages* p, PagesView* pg, bool pointers) {
   if (!p || p->n_units < 0) return CASK_EINVAL;
@@ -281,12 +285,12 @@ static int resolve_pages(const KParams& kp, const cask_pages* p, PagesView* pg, 
   pg->table = p->table;
   if (p->table) {
     if (p->page_rows < 16 || p->page_rows > (1 << 20) || (p->page_rows & (p->page_rows - 1)) || p->table_pitch < 1) return CASK_EINVAL;
-    if ((int64_t)p->table_pitch * p->page_rows > (1 << 30)) return CASK_EINVAL;
+    if ((int64_t)p->table_pitch * p->page_rows > kMostUnitRows) return CASK_EINVAL;
     pg->shift = __builtin_ctz((unsigned)p->page_rows);
     pg->mask = p->page_rows - 1;
     pg->cap = p->table_pitch * p->page_rows;
   } else {
-    if (p->page_rows > (1 << 30) || p->n_pages < p->n_units) return CASK_EINVAL;
+    if (p->page_rows > kMostUnitRows || p->n_pages < p->n_units) return CASK_EINVAL;
     if (p->type == CASK_E4M3 && p->page_rows % 16) return CASK_EINVAL;
     pg->shift = 31;
     pg->mask = 0x7fffffff;
@@ -306,7 +310,7 @@ static int resolve_pages(const KParams& kp, const cask_pages* p, PagesView* pg, 
 
 static int resolve_rows(const KParams& kp, const PagesView& pg, const cask_rows* r, RowsView* rw, bool pointers) {
   if (!r || r->max_n < 0 || r->pitch < 1 || r->total < 0 || r->total > (1ll << 40)) return CASK_EINVAL;
-  if ((int64_t)r->max_n * kp.G > (1 << 30) || (int64_t)r->max_n * pg.n_units > 0x7fffffffll) return CASK_EINVAL;
+  if ((int64_t)r->max_n * kp.G > kMostUnitRows || (int64_t)r->max_n * pg.n_units > 0x7fffffffll) return CASK_EINVAL;
   if (pointers && pg.n_units > 0 && r->max_n > 0 && !r->n) return CASK_EINVAL;
   rw->max_n = r->max_n;
   rw->pitch = r->pitch;
@@ -558,6 +562,7 @@ int cask_attend_paged(const cask_params* params, const cask_pages* pages, const 
   const int rc = resolve_paged(params, pages, rows, &kp, &pa.pg, &pa.rw, true, &none);
   if (rc) return rc;
   if (window < 0 || sinks < 0 || max_rows < 0 || (count && count_pitch < 1)) return CASK_EINVAL;
+  if (!paged_fits(kp, pa.pg.n_units, pa.rw.max_n)) return CASK_EINVAL;
   if (none) return CASK_OK;
   if (!Q || !out || misaligned16(Q) || misaligned16(out) || misaligned16(ws)) return CASK_EINVAL;
   const bool e4m3 = pages->type == CASK_E4M3;
@@ -565,8 +570,8 @@ int cask_attend_paged(const cask_params* params, const cask_pages* pages, const 
   pa.out = out;
   pa.count = count;
   pa.count_pitch = count_pitch;
-  pa.window = window;
-  pa.sinks = sinks;
+  pa.window = window < (1 << 30) ? window : (1 << 30);
+  pa.sinks = sinks < (1 << 30) ? sinks : (1 << 30);
   pa.part = static_cast<float*>(ws);
   const int most = paged_max_rows(pa.pg, max_rows);
   const PagedPlan plan = paged_plan(kp, pa.pg.n_units, pa.rw.max_n, e4m3, window, sinks, most);
@@ -582,7 +587,7 @@ size_t cask_attend_paged_workspace_bytes(const cask_params* params, const cask_p
   RowsView rw;
   bool none;
   if (resolve_paged(params, pages, rows, &kp, &pg, &rw, false, &none) != CASK_OK || none) return 0;
-  if (window < 0 || sinks < 0 || max_rows < 0) return 0;
+  if (window < 0 || sinks < 0 || max_rows < 0 || !paged_fits(kp, pg.n_units, rw.max_n)) return 0;
   return paged_part_bytes(kp, pg.n_units, rw.max_n,
                           paged_plan(kp, pg.n_units, rw.max_n, pages->type == CASK_E4M3, window, sinks, paged_max_rows(pg, max_rows)).splits);
 }

@@ -391,7 +391,7 @@ __device__ inline int rows_of_unit(const RowsView& rw, int u) {
 __device__ inline int64_t first_of_unit(const RowsView& rw, int u) {
   return rw.first ? rw.first[u] : (int64_t)u * rw.max_n;
 }
-// Place of row t of the call in its arrays, -1 if that is outside them (no product or sum here wraps: 0 <= t < 2^30,
+// Place of row t of the call in its arrays, -1 if that is outside them (no product or sum here wraps: 0 <= t < 2^29,
 // and a row this far on is compared before it is multiplied).
 __device__ inline int64_t array_row(const RowsView& rw, int64_t first, int t) {
   if (first < 0 || first >= rw.total) return -1;
@@ -424,6 +424,8 @@ struct PagedAttend {
   int splits;         // workgroups that share the rows of a block of queries
   float* part;        // their partial results
 };
+// Whether the launches of such a call stay below 2^32 threads.
+bool paged_fits(const KParams& kp, int n_units, int max_n);
 // How such a call is done (max_rows: about the largest number of rows a unit holds), and the bytes of its splits' results.
 struct PagedPlan {
   bool chunk;  // blocks of 256 query rows, else of 16 or 32

@@ -116,7 +116,7 @@ __device__ inline float quantise(const Share<T, N>& x, uint32_t (&q)[N / 4]) {
 struct RowPlace {
   int64_t array, pool;  // -1: none
 };
-__device__ inline RowPlace place_of(const PagesView& pg, const RowsView& rw, int64_t item) {
+__device__ inline RowPlace place_of(const PagesView& pg, const RowsView& rw, int64_t item) {  // item < 2^31, see resolve_rows
   RowPlace at{-1, -1};
   if (item >= (int64_t)pg.n_units * rw.max_n) return at;
   const int u = (int)((uint32_t)item / (uint32_t)rw.max_n), t = (int)((uint32_t)item % (uint32_t)rw.max_n);
@@ -133,28 +133,31 @@ __global__ __launch_bounds__(256) void cache_write_kernel(PagesView pg, RowsView
                                                           const T* __restrict__ V) {
   constexpr int N = D / kRowLanes;
   const int lane = threadIdx.x % kRowLanes;
-  const RowPlace at = place_of(pg, rw, (int64_t)blockIdx.x * kBlockRows + threadIdx.x / kRowLanes);
-  if (at.array < 0 || at.pool < 0) return;  // (the lanes of a row leave together)
-  Share<T, N> k, v;
-  k.load(K + at.array * D + lane * N);
-  v.load(V + at.array * D + lane * N);
-  if constexpr (E4M3) {
-    uint32_t qk[N / 4], qv[N / 4];
-    const float sk = quantise(k, qk), sv = quantise(v, qv);
-    Share<uint8_t, N> out;
+  const int64_t items = (int64_t)pg.n_units * rw.max_n;
+  for (int64_t item = (int64_t)blockIdx.x * kBlockRows + threadIdx.x / kRowLanes; item < items; item += (int64_t)gridDim.x * kBlockRows) {
+    const RowPlace at = place_of(pg, rw, item);
+    if (at.array < 0 || at.pool < 0) continue;  // (the lanes of a row go on together)
+    Share<T, N> k, v;
+    k.load(K + at.array * D + lane * N);
+    v.load(V + at.array * D + lane * N);
+    if constexpr (E4M3) {
+      uint32_t qk[N / 4], qv[N / 4];
+      const float sk = quantise(k, qk), sv = quantise(v, qv);
+      Share<uint8_t, N> out;
 #pragma unroll
-    for (int i = 0; i < N / 4; ++i) out.w[i] = qk[i];
-    out.store(pg.K + at.pool * D + lane * N);
+      for (int i = 0; i < N / 4; ++i) out.w[i] = qk[i];
+      out.store(pg.K + at.pool * D + lane * N);
 #pragma unroll
-    for (int i = 0; i < N / 4; ++i) out.w[i] = qv[i];
-    out.store(pg.V + at.pool * D + lane * N);
-    if (lane == 0) {
-      pg.K_scale[at.pool] = sk;
-      pg.V_scale[at.pool] = sv;
+      for (int i = 0; i < N / 4; ++i) out.w[i] = qv[i];
+      out.store(pg.V + at.pool * D + lane * N);
+      if (lane == 0) {
+        pg.K_scale[at.pool] = sk;
+        pg.V_scale[at.pool] = sv;
+      }
+    } else {
+      k.store(reinterpret_cast<T*>(pg.K) + at.pool * D + lane * N);
+      v.store(reinterpret_cast<T*>(pg.V) + at.pool * D + lane * N);
     }
-  } else {
-    k.store(reinterpret_cast<T*>(pg.K) + at.pool * D + lane * N);
-    v.store(reinterpret_cast<T*>(pg.V) + at.pool * D + lane * N);
   }
 }
 
@@ -180,35 +183,40 @@ template <typename T, bool E4M3, int D>
 __global__ __launch_bounds__(256) void cache_read_kernel(PagesView pg, RowsView rw, T* __restrict__ K, T* __restrict__ V) {
   constexpr int N = D / kRowLanes;
   const int lane = threadIdx.x % kRowLanes;
-  const RowPlace at = place_of(pg, rw, (int64_t)blockIdx.x * kBlockRows + threadIdx.x / kRowLanes);
-  if (at.array < 0) return;
-  Share<T, N> k, v;
+  const int64_t items = (int64_t)pg.n_units * rw.max_n;
+  for (int64_t item = (int64_t)blockIdx.x * kBlockRows + threadIdx.x / kRowLanes; item < items; item += (int64_t)gridDim.x * kBlockRows) {
+    const RowPlace at = place_of(pg, rw, item);
+    if (at.array < 0) continue;
+    Share<T, N> k, v;
 #pragma unroll
-  for (int i = 0; i < k.kWords; ++i) k.w[i] = v.w[i] = 0u;
-  if (at.pool >= 0) {
-    if constexpr (E4M3) {
-      uint32_t qk[N / 4], qv[N / 4];
-      const uint32_t* pk = reinterpret_cast<const uint32_t*>(pg.K + at.pool * D + lane * N);
-      const uint32_t* pv = reinterpret_cast<const uint32_t*>(pg.V + at.pool * D + lane * N);
+    for (int i = 0; i < k.kWords; ++i) k.w[i] = v.w[i] = 0u;
+    if (at.pool >= 0) {
+      if constexpr (E4M3) {
+        uint32_t qk[N / 4], qv[N / 4];
+        const uint32_t* pk = reinterpret_cast<const uint32_t*>(pg.K + at.pool * D + lane * N);
+        const uint32_t* pv = reinterpret_cast<const uint32_t*>(pg.V + at.pool * D + lane * N);
 #pragma unroll
-      for (int i = 0; i < N / 4; ++i) {
-        qk[i] = pk[i];
-        qv[i] = pv[i];
+        for (int i = 0; i < N / 4; ++i) {
+          qk[i] = pk[i];
+          qv[i] = pv[i];
+        }
+        const float sk = pg.K_scale[at.pool], sv = pg.V_scale[at.pool];
+        widen<T, N>(qk, sk, k);
+        widen<T, N>(qv, sv, v);
+      } else {
+        k.load(reinterpret_cast<const T*>(pg.K) + at.pool * D + lane * N);
+        v.load(reinterpret_cast<const T*>(pg.V) + at.pool * D + lane * N);
       }
-      const float sk = pg.K_scale[at.pool], sv = pg.V_scale[at.pool];
-      widen<T, N>(qk, sk, k);
-      widen<T, N>(qv, sv, v);
-    } else {
-      k.load(reinterpret_cast<const T*>(pg.K) + at.pool * D + lane * N);
-      v.load(reinterpret_cast<const T*>(pg.V) + at.pool * D + lane * N);
     }
+    k.store(K + at.array * D + lane * N);
+    v.store(V + at.array * D + lane * N);
   }
-  k.store(K + at.array * D + lane * N);
-  v.store(V + at.array * D + lane * N);
 }
 
+// Workgroups of a call; they go round again where there would be 2^32 threads.
 int row_blocks(const PagesView& pg, const RowsView& rw) {
-  return (int)(((int64_t)pg.n_units * rw.max_n + kBlockRows - 1) / kBlockRows);
+  const int64_t blocks = ((int64_t)pg.n_units * rw.max_n + kBlockRows - 1) / kBlockRows;
+  return (int)(blocks < (1 << 23) ? blocks : (1 << 23));
 }
 
 }  // namespace

@@ -1106,6 +1106,7 @@ __global__ __launch_bounds__(512, 2) void paged_chunk_kernel(ChunkParams kp, Pag
           }
       }
     }
+    __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): the requests of stages behind the last
     if (grown_prev) rescale(corr);
 #pragma unroll
     for (int cb = 0; cb < CB; ++cb) {
@@ -1201,6 +1202,15 @@ hipError_t launch_combine(const KParams& kp, const PagedAttend& pa, hipStream_t 
 
 }  // namespace
 
+// Blocks of queries that a launch may have: below 2^32 threads.
+constexpr int64_t kMostBlocks = 1 << 22;
+static int64_t query_blocks(const KParams& kp, int n_units, int max_n, int64_t block) {
+  return (int64_t)n_units * (((int64_t)max_n * kp.G + block - 1) / block);
+}
+bool paged_fits(const KParams& kp, int n_units, int max_n) {
+  return query_blocks(kp, n_units, max_n, kp.dtype == CASK_F32 ? kCols : ChunkGeom<128>::kBlockQ) <= kMostBlocks;
+}
+
 // Which kernel, and how many workgroups share the rows of a block of queries.  By what a call takes, as measured (us):
 // rounds of the 256 compute units, each `start` + `row` for every row that a workgroup goes through; with splits 4 for
 // the launch that adds them and their results' way to memory and back at 4 TB/s.
@@ -1216,14 +1226,13 @@ PagedPlan paged_plan(const KParams& kp, int n_units, int max_n, bool e4m3, int w
   const int64_t m = (int64_t)max_n * kp.G;
   const bool f32 = kp.dtype == CASK_F32, wide = kp.d == 128;
   auto cost = [&](int64_t block, int least, double start, double per_row, int* splits) {
-    const int64_t blocks = (int64_t)n_units * ((m + block - 1) / block);
+    const int64_t blocks = query_blocks(kp, n_units, max_n, block);
     int64_t rows = max_rows;
     const int64_t tokens = (block < m ? block : m) / kp.G + 1;
     if (window > 0 && window + tokens + sinks < rows) rows = window + tokens + sinks;
     double best = 0.0;
     for (int s = 1; s <= kMostSplits && (s == 1 || rows >= (int64_t)s * least); ++s) {
-      // (a split's launch counts workgroups in 31 bits, the one behind it query rows)
-      if (s > 1 && (blocks * s > (1 << 28) || n_units * m > (1 << 28))) break;
+      if (s > 1 && (blocks * s > kMostBlocks || n_units * m > kMostBlocks)) break;
       double c = (double)((blocks * s + 255) / 256) * (start + per_row * 1e-3 * (double)((rows + s - 1) / s));
       if (s > 1) c += 4.0 + (double)n_units * m * s * kp.d * 8.0 / 4.0e6;
       if (s == 1 || c < best) best = c, *splits = s;
@@ -1234,9 +1243,10 @@ PagedPlan paged_plan(const KParams& kp, int n_units, int max_n, bool e4m3, int w
   const bool two = m > kCols && (!f32 || !wide);
   const double c_few = cost(two ? 2 * kCols : kCols, 256, 4.0, f32 ? 32.0 : two ? (wide ? 15.5 : 9.0) : (wide ? 9.0 : 5.0), &few.splits);
   const bool ask_many = (kp.path_flags & CASK_PATH_PAGED_MANY) != 0, ask_few = (kp.path_flags & CASK_PATH_PAGED_FEW) != 0;
-  if (f32 || ask_few || (m <= 2 * kCols && !ask_many)) return few;
+  const bool few_fit = query_blocks(kp, n_units, max_n, kCols) <= kMostBlocks;
+  if (f32 || (few_fit && (ask_few || (m <= 2 * kCols && !ask_many)))) return few;
   const double c_many = cost(ChunkGeom<128>::kBlockQ, 128, 6.0, wide ? (e4m3 ? 45.0 : 36.0) : (e4m3 ? 27.0 : 23.0), &many.splits);
-  return c_many < c_few || ask_many ? many : few;
+  return c_many < c_few || ask_many || !few_fit ? many : few;
 }
 
 size_t paged_part_bytes(const KParams& kp, int n_units, int max_n, int splits) {

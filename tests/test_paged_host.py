@@ -77,6 +77,18 @@ def test_arguments_that_are_refused(lib):
     assert _calls(lib, p=cask.Params(head_dim=96, window=1, budget=2)) == (B.EINVAL,) * 3
 
 
+def test_launches_that_would_have_too_many_threads(lib):
+    """More query blocks than a launch may have: refused by the attention; fp32's blocks are the smaller ones."""
+    big = dict(pages=_pages(n_units=1 << 15), rows=_rows(max_n=1 << 15, total=1 << 30))
+    for G, dtype, bad in ((4, B.F32, True), (2, B.BF16, True), (1, B.BF16, False)):
+        p = cask.Params(dtype=dtype, q_per_kv=G, window=1, budget=2)
+        pages = _pages(n_units=1 << 15, type=dtype)
+        need = lib.cask_attend_paged_workspace_bytes(C.byref(p.c()), C.byref(pages), C.byref(big["rows"]), 0, 0, 0)
+        assert need == 0
+        if bad:
+            assert _calls(lib, p=p, pages=pages, rows=big["rows"])[2] == B.EINVAL
+
+
 def test_nothing_to_do_touches_nothing(lib):
     """No units, no rows, no arrays: fine, whatever the pointers."""
     nothing = dict(K=None, V=None)
