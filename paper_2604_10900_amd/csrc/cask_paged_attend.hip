@@ -747,13 +747,14 @@ __global__ __launch_bounds__(512, 2) void paged_chunk_kernel(ChunkParams kp, Pag
     const int s = s0 + lane, r = stage_row(s) + wv * 8;
     entries = -1;
     if (s < n_stages && r < ur.end) entries = pa.pg.table ? pa.pg.table[(int64_t)u * pa.pg.table_pitch + (r >> pa.pg.shift)] : u;
+    asm volatile("" : "+v"(entries));  // (the wait for them here, or every stage waits for all loads under way before it reads one)
   };
   struct Place {
     int64_t at;  // pool row of the first of the wave's rows of a stage
     int rows;    // how many are there
   };
-  auto find = [&](int s) {
-    const int e = __builtin_amdgcn_readlane(entries, s & 63), r = stage_row(s) + wv * 8;
+  auto find = [&](int s, int r_stage) {
+    const int e = __builtin_amdgcn_readlane(entries, s & 63), r = r_stage + wv * 8;
     Place p{0, 0};
     if ((unsigned)e < (unsigned)pa.pg.n_pages) p = Place{e * pa.pg.pitch + (r & pa.pg.mask), min(8, ur.end - r)};
     // (bit o of a stage's eight bytes: row o of it is there; read by all waves a stage before its own)
@@ -768,18 +769,17 @@ __global__ __launch_bounds__(512, 2) void paged_chunk_kernel(ChunkParams kp, Pag
   auto buffer = [&](const void* base, int64_t at, int bytes) {
     return __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<unsigned char*>(const_cast<void*>(base)) + at, 0, __builtin_amdgcn_readfirstlane(bytes), 0x00020000u);
   };
-  auto lds_address = [](const void* p) {
-    return __builtin_amdgcn_readfirstlane((int)(uintptr_t)(__attribute__((address_space(3))) const unsigned char*)p);
-  };
+  // (places in LDS as numbers: a generic pointer is tested for null at every use)
+  const int ring_lds = __builtin_amdgcn_readfirstlane((int)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)ring);
   // A kilobyte to LDS, sixteen bytes a lane.  (Written out because the compiler lets every transposing read wait for
   // all such loads that it knows of: a chunk of 2048 x 7 query rows behind 16 384 rows took 695 us so and 559 without
   // that wait.  The waits are in `meet`; the loads return no register.)
-  auto load_lds = [&](unsigned char* dst, u32x4 rs, int off) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds_address(dst)), "v"(off), "s"(rs) : "memory");
+  auto load_lds = [&](int dst, u32x4 rs, int off) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(__builtin_amdgcn_readfirstlane(dst)), "v"(off), "s"(rs) : "memory");
   };
   // bf16: straight to LDS, a KB an instruction.  Lane -> group of four rows, piece, row of the group as they lie there.
   constexpr int kLoads = 8 * D / 512, kGroupLanes = D / 2;   // instructions of eight rows; lanes of a group
-  auto load_rows = [&](unsigned char* dst, const unsigned char* pool, const Place& p) {
+  auto load_rows = [&](int dst, const unsigned char* pool, const Place& p) {
     const u32x4 rs = rsrc_of(pool, p.at * ROWB, p.rows * ROWB);
 #pragma unroll
     for (int j = 0; j < kLoads; ++j) {
@@ -789,38 +789,42 @@ __global__ __launch_bounds__(512, 2) void paged_chunk_kernel(ChunkParams kp, Pag
     }
   };
   auto slot_at = [&](int s) { return ring + (s & (A::kDepth - 1)) * A::kSlot; };
-  auto load_counts = [&](int s) {  // of a stage's rows, by one of the waves
-    const int r = stage_row(s);
-    if (!cu || s >= n_stages || r >= pa.count_pitch || wv != (s & 7)) return;
-    const u32x4 rs = rsrc_of(cu, (int64_t)r * 4, min(pa.count_pitch - r, A::kStage) * 4);  // (behind them: 0, which counts as one)
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(lds_address(aux_all + (s & (A::kDepth - 1)) * A::kAux)),
+  auto slot_lds = [&](int s) { return ring_lds + (s & (A::kDepth - 1)) * A::kSlot; };
+  constexpr int kAuxAt = A::kDepth * A::kSlot, kRawAt = kAuxAt + A::kDepth * (A::kAux * 4 + 8) + A::kWaves * 64 * A::kMarks * 4;
+  auto load_counts = [&](int s, int r_stage) {  // of a stage's rows, by one of the waves
+    if (s >= n_stages || r_stage >= pa.count_pitch || wv != (s & 7)) return;
+    const u32x4 rs = rsrc_of(cu, (int64_t)r_stage * 4, min(pa.count_pitch - r_stage, A::kStage) * 4);  // (behind them: 0, which counts as one)
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(__builtin_amdgcn_readfirstlane(ring_lds + kAuxAt + (s & (A::kDepth - 1)) * A::kAux * 4)),
                  "v"(lane * 4), "s"(rs) : "memory");
   };
   // Counts of stage s into their logarithms, a stage before it: by the wave that asked for them, once they are there (bf16:
   // `meet` has waited, e4m3: commit).
   auto convert_counts = [&](int s) {
-    if (!cu || s >= n_stages || stage_row(s) >= pa.count_pitch || wv != (s & 7)) return;
+    if (s >= n_stages || stage_row(s) >= pa.count_pitch || wv != (s & 7)) return;
     float* at = aux_all + (s & (A::kDepth - 1)) * A::kAux + lane;
     asm volatile("" ::: "memory");
     *at = __builtin_amdgcn_logf((float)max((int)__float_as_uint(*at), 1));
   };
-  auto load_keys = [&](int s, const Place& p) {
-    load_counts(s);
-    load_rows(slot_at(s) + wv * 8 * A::kRowB, pa.pg.K, p);
+  auto load_keys = [&](int s, int r_stage, const Place& p) {
+    if (cu) load_counts(s, r_stage);
+    load_rows(slot_lds(s) + wv * 8 * A::kRowB, pa.pg.K, p);
   };
-  auto load_values = [&](int s, const Place& p) { load_rows(slot_at(s) + A::kSlotK + wv * 8 * A::kRowB, pa.pg.V, p); };
+  auto load_values = [&](int s, const Place& p) { load_rows(slot_lds(s) + A::kSlotK + wv * 8 * A::kRowB, pa.pg.V, p); };
   // e4m3: sixteen bytes a lane to a place of the wave's own in LDS, a stage later from there into the ring as bf16
-  // (held in registers until then they made the wave spill others)
+  // (held in registers until then they made the wave spill others).  Lane l brings piece l / 8 of row l % 8: eight lanes
+  // then write 128 bytes of the ring that lie together (a row's lanes next to each other: an eight-way bank conflict).
   constexpr int kLanesPerRow = D / 16;              // lanes that share a row
   constexpr bool kWhole = 8 * kLanesPerRow == 64;  // (64 channels: half of the lanes)
   uint32_t a_ks = 0u, a_vs = 0u;                    // scales of row lane % 8 of the wave's eight
   auto issue = [&](int s) {
-    const Place p = find(s);
-    load_counts(s);
+    const int r_stage = stage_row(s);
+    const Place p = find(s, r_stage);
+    if (cu) load_counts(s, r_stage);
     __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0): what commit read from there has been read
+    const int off = (lane & 7) * ROWB + (lane >> 3) * 16;
     if (kWhole || lane < 8 * kLanesPerRow) {
-      load_lds(raw_all + wv * 8 * D, rsrc_of(pa.pg.K, p.at * ROWB, p.rows * ROWB), lane * 16);
-      load_lds(raw_all + A::kRaw + wv * 8 * D, rsrc_of(pa.pg.V, p.at * ROWB, p.rows * ROWB), lane * 16);
+      load_lds(ring_lds + kRawAt + wv * 8 * D, rsrc_of(pa.pg.K, p.at * ROWB, p.rows * ROWB), off);
+      load_lds(ring_lds + kRawAt + A::kRaw + wv * 8 * D, rsrc_of(pa.pg.V, p.at * ROWB, p.rows * ROWB), off);
     }
     a_ks = __builtin_amdgcn_raw_buffer_load_b32(buffer(pa.pg.K_scale, p.at * 4, p.rows * 4), (lane & 7) * 4, 0, 0);   // (behind the rows: 0)
     a_vs = __builtin_amdgcn_raw_buffer_load_b32(buffer(pa.pg.V_scale, p.at * 4, p.rows * 4), (lane & 7) * 4, 0, 0);
@@ -836,11 +840,11 @@ __global__ __launch_bounds__(512, 2) void paged_chunk_kernel(ChunkParams kp, Pag
       aux[A::kStage + lane] = ks;
       aux[2 * A::kStage + lane] = fabsf(vs) < __builtin_inff() ? vs : 0.f;
     }
-    convert_counts(s);
+    if (cu) convert_counts(s);
     unsigned char* slot = slot_at(s);
-    const int r = wv * 8 + lane / kLanesPerRow, piece = (lane % kLanesPerRow) * 2;
+    const int r = wv * 8 + (lane & 7), piece = (lane >> 3) * 2;
     // a row of values whose scale is not finite lies there as a row of NaN with a scale of zero
-    const bool lost = !(fabsf(__shfl(vs, lane / kLanesPerRow, 64)) < __builtin_inff());
+    const bool lost = !(fabsf(vs) < __builtin_inff());
     if (lane < 8 * kLanesPerRow) {
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
@@ -917,12 +921,12 @@ __global__ __launch_bounds__(512, 2) void paged_chunk_kernel(ChunkParams kp, Pag
   // A tile that some query does not see whole: values that are not finite out of the product, and marks for those
   // that see one.
   auto clean = [&](bf16x8 (&a)[2], uint32_t bits, int cb) {  // (bits: seen_bits of the tile; rows that are not there hold zeros)
-    uint32_t odd = 0u;
+    uint32_t odd = 0u;  // (bits 15 and 31 alone: see not_finite2)
 #pragma unroll
     for (int m = 0; m < 2; ++m)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) odd |= not_finite2(__builtin_bit_cast(u32x4, a[m])[e]);
-    if (!__any(odd != 0u)) return;
+      for (int e = 0; e < 4; ++e) odd |= (__builtin_bit_cast(u32x4, a[m])[e] & 0x7f807f80u) + 0x00800080u;
+    if (!__any((odd & 0x80008000u) != 0u)) return;
     f32x16 seen;
 #pragma unroll
     for (int i = 0; i < 16; ++i) seen[i] = 0.f;
@@ -1018,19 +1022,20 @@ __global__ __launch_bounds__(512, 2) void paged_chunk_kernel(ChunkParams kp, Pag
       commit(1);
       issue(2);
     } else {
-      const Place p0 = find(0), p1 = find(1);
-      load_keys(0, p0);
+      const Place p0 = find(0, stage_row(0)), p1 = find(1, stage_row(1));
+      load_keys(0, stage_row(0), p0);
       load_values(0, p0);
-      load_keys(1, p1);
-      next_v = find(2);
-      load_keys(2, next_v);
+      load_keys(1, stage_row(1), p1);
+      next_v = find(2, stage_row(2));
+      load_keys(2, stage_row(2), next_v);
       load_values(1, p1);
     }
     meet();
-    if constexpr (!E4M3) {
-      convert_counts(0);
-      if (cu) meet();
-    }
+    if constexpr (!E4M3)
+      if (cu) {
+        convert_counts(0);
+        meet();
+      }
     bf16x8 a[NK];
     load_k(a, 0, 0);
     logits(s[0], a);
@@ -1051,11 +1056,12 @@ __global__ __launch_bounds__(512, 2) void paged_chunk_kernel(ChunkParams kp, Pag
       flag_next = flags_of(after);
       if (((st + 3) & 63) == 0) load_entries(st + 3);
       if constexpr (!E4M3) {
-        const Place next_k = find(st + 3);
-        load_keys(st + 3, next_k);
+        const int r_next = stage_row(st + 3);
+        const Place next_k = find(st + 3, r_next);
+        load_keys(st + 3, r_next, next_k);
         load_values(st + 2, next_v);
         next_v = next_k;
-        convert_counts(st + 1);
+        if (cu) convert_counts(st + 1);
       }
       const bool counted = cu && r_stage < pa.count_pitch;
 #pragma unroll
