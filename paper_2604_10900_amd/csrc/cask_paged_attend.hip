@@ -1054,15 +1054,6 @@ __global__ __launch_bounds__(512, 2) void paged_chunk_kernel(ChunkParams kp, Pag
       const int r_stage = stage_row(st);
       const uint32_t here[2] = {(uint32_t)__builtin_amdgcn_readfirstlane((int)flag_next[0]), (uint32_t)__builtin_amdgcn_readfirstlane((int)flag_next[1])};
       flag_next = flags_of(after);
-      if (((st + 3) & 63) == 0) load_entries(st + 3);
-      if constexpr (!E4M3) {
-        const int r_next = stage_row(st + 3);
-        const Place next_k = find(st + 3, r_next);
-        load_keys(st + 3, r_next, next_k);
-        load_values(st + 2, next_v);
-        next_v = next_k;
-        if (cu) convert_counts(st + 1);
-      }
       const bool counted = cu && r_stage < pa.count_pitch;
 #pragma unroll
       for (int half = 0; half < 2; ++half) {
@@ -1072,6 +1063,21 @@ __global__ __launch_bounds__(512, 2) void paged_chunk_kernel(ChunkParams kp, Pag
 #pragma unroll
         for (int cb = 0; cb < CB; ++cb) load_v(v[cb], half ? place : before, half ^ (st > 0 || half), cb);
         logits(s[half ^ 1], a);
+        // what brings rows, while the matrix cores work on the logits
+        if (half == (E4M3 ? 1 : 0)) {
+          if (((st + 3) & 63) == 0) load_entries(st + 3);
+          if constexpr (E4M3) {
+            commit(st + 2);
+            issue(st + 3);
+          } else {
+            const int r_next = stage_row(st + 3);
+            const Place next_k = find(st + 3, r_next);
+            load_keys(st + 3, r_next, next_k);
+            load_values(st + 2, next_v);
+            next_v = next_k;
+            if (cu) convert_counts(st + 1);
+          }
+        }
         exponents(place, half, s[half]);
         if (at_edge || counted || here[half] != ~0u) mask(place, half, r, s[half], here[half], counted);
         float mx = s[half][0];
@@ -1105,11 +1111,6 @@ __global__ __launch_bounds__(512, 2) void paged_chunk_kernel(ChunkParams kp, Pag
         l = __builtin_fmaf(l, grown_prev ? corr : 1.f, ps);
         edge_prev = at_edge;
         r_prev = r;
-        if constexpr (E4M3)
-          if (half == 0) {
-            commit(st + 2);
-            issue(st + 3);
-          }
       }
     }
     __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): the requests of stages behind the last
