@@ -667,7 +667,8 @@ struct ChunkGeom {
   static constexpr int kWaveQ = 32, kWaves = 8, kBlockQ = kWaveQ * kWaves;  // query rows of a wave, of a workgroup
   static constexpr int kStage = 64;                     // cache rows of a ring slot, eight from each wave
   static constexpr int kRowB = D * 2;                   // bytes of a row in LDS: bf16
-  static constexpr int kSlotK = kStage * kRowB;         // keys of a slot; its values lie behind them
+  static constexpr int kEight = 8 * kRowB + 128;        // bytes of the eight rows that a wave brings
+  static constexpr int kSlotK = kWaves * kEight;        // keys of a slot; its values lie behind them
   static constexpr int kSlot = 2 * kSlotK;
   static constexpr int kDepth = 4;
   static constexpr int kAux = kStage * 3;               // words of a slot: count, later its logarithm, key scale, value scale of a row
@@ -675,10 +676,13 @@ struct ChunkGeom {
   static constexpr int kMarks = (D + 63) / 64;          // words of a lane
   static constexpr int kLds = kDepth * (kSlot + kAux * 4 + 8) + kWaves * 64 * kMarks * 4, kLdsE4m3 = kLds + 2 * kRaw;
   // Rows lie in LDS in groups of four, the group's 16-byte pieces one behind the other, each of them for its four
-  // rows; every other group has its neighbouring pieces swapped.  Eight rows' reads of one piece (keys), and four
-  // rows' reads of two neighbouring pieces (values), then meet 128 bytes that lie together.
+  // rows; every other group has its neighbouring pieces swapped, and 128 bytes stay free behind every other one.
+  // Sixteen rows' reads of one piece (keys), and four rows' reads of four neighbouring pieces (values), then meet all
+  // 256 bytes that the banks give in a cycle.  (Keys without the free bytes: 8 cycles a read for 4, and 533 us for 528
+  // of 2048 x 7 query rows behind 16 384 rows; an e4m3 cache waits for its conversions and has no gain from them.)
   __device__ static int place(int row, int piece) {
-    return (row >> 2) * (4 * kRowB) + ((piece ^ ((row >> 2) & 1)) * 4 + (row & 3)) * 16;
+    const int odd = (row >> 2) & 1;
+    return (row >> 3) * kEight + odd * (4 * kRowB) + ((piece ^ odd) * 4 + (row & 3)) * 16;
   }
 };
 
@@ -773,8 +777,8 @@ __global__ __launch_bounds__(512, 2) void paged_chunk_kernel(ChunkParams kp, Pag
   // (places in LDS as numbers: a generic pointer is tested for null at every use)
   const int ring_lds = __builtin_amdgcn_readfirstlane((int)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)ring);
   // A kilobyte to LDS, sixteen bytes a lane.  (Written out because the compiler lets every transposing read wait for
-  // all such loads that it knows of: a chunk of 2048 x 7 query rows behind 16 384 rows took 695 us so and 559 without
-  // that wait.  The waits are in `meet`; the loads return no register.)
+  // all such loads that it knows of: as measured when this was written, a chunk of 2048 x 7 query rows behind 16 384 rows took
+  // 695 us so and 559 without that wait.  The waits are in `meet`; the loads return no register.)
   auto load_lds = [&](int dst, u32x4 rs, int off) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(__builtin_amdgcn_readfirstlane(dst)), "v"(off), "s"(rs) : "memory");
   };
@@ -808,9 +812,9 @@ __global__ __launch_bounds__(512, 2) void paged_chunk_kernel(ChunkParams kp, Pag
   };
   auto load_keys = [&](int s, int r_stage, const Place& p) {
     if (cu) load_counts(s, r_stage);
-    load_rows(slot_lds(s) + wv * 8 * A::kRowB, pa.pg.K, p);
+    load_rows(slot_lds(s) + wv * A::kEight, pa.pg.K, p);
   };
-  auto load_values = [&](int s, const Place& p) { load_rows(slot_lds(s) + A::kSlotK + wv * 8 * A::kRowB, pa.pg.V, p); };
+  auto load_values = [&](int s, const Place& p) { load_rows(slot_lds(s) + A::kSlotK + wv * A::kEight, pa.pg.V, p); };
   // e4m3: sixteen bytes a lane to a place of the wave's own in LDS, a stage later from there into the ring as bf16
   // (held in registers until then they made the wave spill others).  Lane l brings piece l / 8 of row l % 8: eight lanes
   // then write 128 bytes of the ring that lie together (a row's lanes next to each other: an eight-way bank conflict).
@@ -873,19 +877,19 @@ __global__ __launch_bounds__(512, 2) void paged_chunk_kernel(ChunkParams kp, Pag
   const int v_at = A::place(4 * h + (i16 >> 2), 2 * half16 + ((i16 & 3) >> 1)) + 8 * (i16 & 1);
   // (a tile is named by its stage's place in the ring, in slots, and its half)
   auto load_k = [&](bf16x8 (&a)[NK], int place, int half) {
-    const unsigned char* p = ring + place * A::kSlot + half * 32 * A::kRowB + k_at;
+    const unsigned char* p = ring + place * A::kSlot + half * 4 * A::kEight + k_at;
 #pragma unroll
     for (int k = 0; k < NK; ++k) a[k] = *reinterpret_cast<const bf16x8*>(p + k * 128);
   };
   auto load_v = [&](bf16x8 (&a)[2], int place, int half, int cb) {
-    const unsigned char* p = ring + place * A::kSlot + A::kSlotK + half * 32 * A::kRowB + v_at;
+    const unsigned char* p = ring + place * A::kSlot + A::kSlotK + half * 4 * A::kEight + v_at;
 #pragma unroll
     for (int m = 0; m < 2; ++m) {
       union { s16x4 s[2]; bf16x8 b; } x;
 #pragma unroll
       for (int e = 0; e < 2; ++e)
         x.s[e] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-            (__attribute__((address_space(3))) s16x4*)(__attribute__((address_space(3))) void*)(p + (4 * m + 2 * e) * (4 * A::kRowB) + cb * 256));
+            (__attribute__((address_space(3))) s16x4*)(__attribute__((address_space(3))) void*)(p + (2 * m + e) * A::kEight + cb * 256));
       a[m] = x.b;
     }
   };
