@@ -196,7 +196,7 @@ def test_plain_attention_is_softmax_over_the_rows_a_query_sees():
                 assert torch.allclose(got[u * 7 + t][0], want[0], rtol=1e-12, atol=1e-12)
 
 
-def test_checker_finds_a_planted_mistake():
+def test_comparison_finds_a_planted_mistake():
     """check_attend passes the rounded result and fails one whose query sees a row too many or too few."""
     pages = _host_cache(dtype="bf16", cache="e4m3", d=128, G=2, units=1, page_rows=16, cap_pages=8, seed=3)
     Q = torch.randn(20, 2, 128, generator=torch.Generator().manual_seed(1)).to(torch.bfloat16)
