@@ -570,13 +570,14 @@ constexpr int kMostSplits = 64, kFewSplits = 8;
 template <typename T, int D>
 __global__ __launch_bounds__(256) void paged_combine_few_kernel(int G, PagedAttend pa, int64_t rows) {
   constexpr int kLanes = D / 4;
-  const int64_t o = (int64_t)blockIdx.x * (256 / kLanes) + threadIdx.x / kLanes, per_unit = (int64_t)pa.rw.max_n * G;
+  const int64_t o = (int64_t)blockIdx.x * (256 / kLanes) + threadIdx.x / kLanes;
   if (o >= rows) return;
   const int ch = (threadIdx.x % kLanes) * 4, S = pa.splits;
-  const int u = (int)(o / per_unit), m = (int)(o % per_unit);
-  if (m >= rows_of_unit(pa.rw, u) * G) return;
+  const uint32_t per_unit = (uint32_t)(pa.rw.max_n * G);  // (no more rows than kMostBlocks in all where there are splits)
+  const int u = (int)((uint32_t)o / per_unit), m = (int)((uint32_t)o % per_unit);
+  // (asked for at once with the partial results, which lie there whether the row exists or not)
+  const bool there = m < rows_of_unit(pa.rw, u) * G;
   const int64_t row = array_row(pa.rw, first_of_unit(pa.rw, u), m / G);
-  if (row < 0) return;
   f32x2 st[kFewSplits];
   f32x4 v[kFewSplits];
   float top = kNegInf;
@@ -595,6 +596,7 @@ __global__ __launch_bounds__(256) void paged_combine_few_kernel(int G, PagedAtte
       num += v[i] * f;
       den = __builtin_fmaf(st[i][1], f, den);
     }
+  if (!there || row < 0) return;
   T* out = static_cast<T*>(pa.out) + (row * G + m % G) * D + ch;
   if constexpr (sizeof(T) == 4) {
     *reinterpret_cast<f32x4*>(out) = f32x4{joined(num[0], den), joined(num[1], den), joined(num[2], den), joined(num[3], den)};
@@ -616,11 +618,11 @@ __global__ __launch_bounds__(256) void paged_combine_kernel(int G, PagedAttend p
   __shared__ float factor[kMost];
   __shared__ float total;
   __shared__ __align__(16) float sums[kGroups][D];
-  const int64_t o = blockIdx.x, per_unit = (int64_t)pa.rw.max_n * G;
-  const int u = (int)(o / per_unit), m = (int)(o % per_unit);
-  if (m >= rows_of_unit(pa.rw, u) * G) return;
+  const int64_t o = blockIdx.x;
+  const uint32_t per_unit = (uint32_t)(pa.rw.max_n * G);
+  const int u = (int)(blockIdx.x / per_unit), m = (int)(blockIdx.x % per_unit);
+  const bool there = m < rows_of_unit(pa.rw, u) * G;  // (see above)
   const int64_t row = array_row(pa.rw, first_of_unit(pa.rw, u), m / G);
-  if (row < 0) return;
   const int S = pa.splits, tid = threadIdx.x, grp = tid / kLanes, ch = (tid % kLanes) * 4;
   if (tid < 64) {
     const f32x2 st = tid < S ? part_state(pa, G, D)[o * S + tid] : f32x2{kNegInf, 0.f};
@@ -644,7 +646,7 @@ __global__ __launch_bounds__(256) void paged_combine_kernel(int G, PagedAttend p
     if (grp + i * kGroups < S) sum += v[i] * factor[grp + i * kGroups];
   *reinterpret_cast<f32x4*>(&sums[grp][ch]) = sum;
   __syncthreads();
-  if (tid < D) {
+  if (there && row >= 0 && tid < D) {
     float num = 0.f;
 #pragma unroll
     for (int g = 0; g < kGroups; ++g) num += sums[g][tid];
