@@ -127,7 +127,7 @@ enum {
   CASK_PATH_NARROW_ROWS = 64, /* both scoring sweeps: 64 resident rows per wave (256 per workgroup) whatever the shape */
   CASK_PATH_WIDE_ROWS = 128,  /* both scoring sweeps: 128 resident rows per wave (512 per workgroup) whatever the shape */
   CASK_PATH_PAGED_FEW = 256,  /* cask_attend_paged: blocks of 16 or 32 query rows whatever the shape */
-  CASK_PATH_PAGED_MANY = 512  /* cask_attend_paged, bf16: blocks of 256 query rows whatever the shape */
+  CASK_PATH_PAGED_MANY = 512  /* cask_attend_paged, bf16: blocks of 256 query rows (64 channels: 128) whatever the shape */
 };
 
 typedef struct {

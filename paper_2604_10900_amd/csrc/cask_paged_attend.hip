@@ -664,13 +664,17 @@ struct ChunkParams {
   float scale_log2;
 };
 
-template <int D>
+template <bool E4M3, int D>
 struct ChunkGeom {
-  static constexpr int kWaveQ = 32, kWaves = 8, kBlockQ = kWaveQ * kWaves;  // query rows of a wave, of a workgroup
-  static constexpr int kStage = 64;                     // cache rows of a ring slot, eight from each wave
+  // 64 channels: four waves, so that two workgroups share a compute unit and one's start and end overlap the other's work
+  // (102 -> 96 us with a window of 512 rows over 4096 tokens, e4m3 turns of conversations 161 -> 147; 128 channels would
+  // need 2 x 137 KB of LDS)
+  static constexpr int kWaveQ = 32, kWaves = D / 16, kBlockQ = kWaveQ * kWaves;  // query rows of a wave, of a workgroup
+  static constexpr int kStage = 64;                     // cache rows of a ring slot
+  static constexpr int kBring = kStage / kWaves;        // of them from each wave: 8 or 16
   static constexpr int kRowB = D * 2;                   // bytes of a row in LDS: bf16
-  static constexpr int kEight = 8 * kRowB + 128;        // bytes of the eight rows that a wave brings
-  static constexpr int kSlotK = kWaves * kEight;        // keys of a slot; its values lie behind them
+  static constexpr int kEight = 8 * kRowB + (E4M3 && D == 64 ? 0 : 128);  // bytes of eight rows
+  static constexpr int kSlotK = kStage / 8 * kEight;        // keys of a slot; its values lie behind them
   static constexpr int kSlot = 2 * kSlotK;
   static constexpr int kDepth = 4;
   static constexpr int kAux = kStage * 3;               // words of a slot: count, later its logarithm, key scale, value scale of a row
@@ -688,7 +692,7 @@ struct ChunkGeom {
   }
 };
 
-// A wave holds 32 query rows in registers, a workgroup of eight waves 256; the cache's rows come through a ring of
+// A wave holds 32 query rows in registers, a workgroup of eight waves 256 (64 channels: of four, 128); the cache's rows come through a ring of
 // 64-row slots in LDS.  Per 32 rows of the cache, on 32x32 matrix tiles:
 //   logits   S[key][query]     = K . Q^T      (lane: query = lane % 32; keys (i & 3) + 8 (i >> 2) + 4 (lane / 32))
 //   values   O[channel][query] += V^T . P     (P as the lane has it: the product's key order is that of S; V^T by
@@ -699,9 +703,12 @@ struct ChunkGeom {
 // the next 32, the weights of these, the values of those before -- so that matrix and vector pipes are both busy.
 // bf16 weights are rounded once (2^-9 of a weight at the most): two terms as for single tokens would cost as many
 // matrix instructions again where these are the bound.
+// Bound: matrix and vector pipes, which a SIMD's two waves keep busy in turn.  2048 x 7 query rows of 4 units behind 16 384 rows:
+// 520 us, 980 TFLOP/s (a library product of 8192^3: 1253); without the exponentials 3 % less, without either product
+// 5 to 13 %: no single part holds it up.
 template <bool E4M3, int D>
-__global__ __launch_bounds__(512, 2) void paged_chunk_kernel(ChunkParams kp, PagedAttend pa, int q_blocks) {
-  using A = ChunkGeom<D>;
+__global__ __launch_bounds__(D * 4, 2) void paged_chunk_kernel(ChunkParams kp, PagedAttend pa, int q_blocks) {
+  using A = ChunkGeom<E4M3, D>;
   constexpr int NK = D / 16, CB = D / 32;
   extern __shared__ __align__(16) unsigned char ring[];
   float* aux_all = reinterpret_cast<float*>(ring + A::kDepth * A::kSlot);
@@ -744,14 +751,15 @@ __global__ __launch_bounds__(512, 2) void paged_chunk_kernel(ChunkParams kp, Pag
     }
   }
 
-  // ---- the ring: wave wv brings rows [8 wv, 8 wv + 8) of a stage, all of one page
+  // ---- the ring: wave wv brings rows [kBring wv, kBring wv + kBring) of a stage, all of one page
+  constexpr int kBring = A::kBring;
   auto stage_row = [&](int s) { return range.tile(s_begin + s) * A::kStage; };
   constexpr int EL = E4M3 ? 1 : 2, ROWB = D * EL;
   // Page of the wave's rows of stage 64 k + lane: one load for 64 stages.  (Looked up at its stage, each entry made
   // the whole wave wait for it.)
   int entries = -1;
   auto load_entries = [&](int s0) {
-    const int s = s0 + lane, r = stage_row(s) + wv * 8;
+    const int s = s0 + lane, r = stage_row(s) + wv * kBring;
     entries = -1;
     if (s < n_stages && r < ur.end) entries = pa.pg.table ? pa.pg.table[(int64_t)u * pa.pg.table_pitch + (r >> pa.pg.shift)] : u;
     asm volatile("" : "+v"(entries));  // (the wait for them here, or every stage waits for all loads under way before it reads one)
@@ -761,11 +769,12 @@ __global__ __launch_bounds__(512, 2) void paged_chunk_kernel(ChunkParams kp, Pag
     int rows;    // how many are there
   };
   auto find = [&](int s, int r_stage) {
-    const int e = __builtin_amdgcn_readlane(entries, s & 63), r = r_stage + wv * 8;
+    const int e = __builtin_amdgcn_readlane(entries, s & 63), r = r_stage + wv * kBring;
     Place p{0, 0};
-    if ((unsigned)e < (unsigned)pa.pg.n_pages) p = Place{e * pa.pg.pitch + (r & pa.pg.mask), min(8, ur.end - r)};
+    if ((unsigned)e < (unsigned)pa.pg.n_pages) p = Place{e * pa.pg.pitch + (r & pa.pg.mask), min(kBring, ur.end - r)};
     // (bit o of a stage's eight bytes: row o of it is there; read by all waves a stage before its own)
-    if (lane == 0) flag_all[(s & (A::kDepth - 1)) * 8 + wv] = (unsigned char)((1 << p.rows) - 1);
+    typedef typename std::conditional<kBring == 8, uint8_t, uint16_t>::type Flags;
+    if (lane == 0) reinterpret_cast<Flags*>(flag_all + (s & (A::kDepth - 1)) * 8)[wv] = (Flags)((1 << p.rows) - 1);
     return p;
   };
   auto rsrc_of = [&](const void* base, int64_t at, int bytes) {  // words of a buffer descriptor
@@ -785,21 +794,21 @@ __global__ __launch_bounds__(512, 2) void paged_chunk_kernel(ChunkParams kp, Pag
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(__builtin_amdgcn_readfirstlane(dst)), "v"(off), "s"(rs) : "memory");
   };
   // bf16: straight to LDS, a KB an instruction.  Lane -> group of four rows, piece, row of the group as they lie there.
-  constexpr int kLoads = 8 * D / 512, kGroupLanes = D / 2;   // instructions of eight rows; lanes of a group
+  constexpr int kLoads = kBring * A::kRowB / 1024, kGroupLanes = D / 2;   // instructions of a wave's rows; lanes of a group
   auto load_rows = [&](int dst, const unsigned char* pool, const Place& p) {
     const u32x4 rs = rsrc_of(pool, p.at * ROWB, p.rows * ROWB);
 #pragma unroll
     for (int j = 0; j < kLoads; ++j) {
       const int grp = j * (64 / kGroupLanes) + lane / kGroupLanes;
       const int piece = (lane % kGroupLanes) / 4 ^ (grp & 1);
-      load_lds(dst + j * 1024, rs, (grp * 4 + lane % 4) * ROWB + piece * 16);
+      load_lds(dst + j * 1024 / (8 * A::kRowB) * A::kEight + j * 1024 % (8 * A::kRowB), rs, (grp * 4 + lane % 4) * ROWB + piece * 16);
     }
   };
   auto slot_at = [&](int s) { return ring + (s & (A::kDepth - 1)) * A::kSlot; };
   auto slot_lds = [&](int s) { return ring_lds + (s & (A::kDepth - 1)) * A::kSlot; };
   constexpr int kAuxAt = A::kDepth * A::kSlot, kRawAt = kAuxAt + A::kDepth * (A::kAux * 4 + 8) + A::kWaves * 64 * A::kMarks * 4;
   auto load_counts = [&](int s, int r_stage) {  // of a stage's rows, by one of the waves
-    if (s >= n_stages || r_stage >= pa.count_pitch || wv != (s & 7)) return;
+    if (s >= n_stages || r_stage >= pa.count_pitch || wv != (s & (A::kWaves - 1))) return;
     const u32x4 rs = rsrc_of(cu, (int64_t)r_stage * 4, min(pa.count_pitch - r_stage, A::kStage) * 4);  // (behind them: 0, which counts as one)
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(__builtin_amdgcn_readfirstlane(ring_lds + kAuxAt + (s & (A::kDepth - 1)) * A::kAux * 4)),
                  "v"(lane * 4), "s"(rs) : "memory");
@@ -807,63 +816,58 @@ __global__ __launch_bounds__(512, 2) void paged_chunk_kernel(ChunkParams kp, Pag
   // Counts of stage s into their logarithms, a stage before it: by the wave that asked for them, once they are there (bf16:
   // `meet` has waited, e4m3: commit).
   auto convert_counts = [&](int s) {
-    if (s >= n_stages || stage_row(s) >= pa.count_pitch || wv != (s & 7)) return;
+    if (s >= n_stages || stage_row(s) >= pa.count_pitch || wv != (s & (A::kWaves - 1))) return;
     float* at = aux_all + (s & (A::kDepth - 1)) * A::kAux + lane;
     asm volatile("" ::: "memory");
     *at = __builtin_amdgcn_logf((float)max((int)__float_as_uint(*at), 1));
   };
   auto load_keys = [&](int s, int r_stage, const Place& p) {
     if (cu) load_counts(s, r_stage);
-    load_rows(slot_lds(s) + wv * A::kEight, pa.pg.K, p);
+    load_rows(slot_lds(s) + wv * (kBring / 8 * A::kEight), pa.pg.K, p);
   };
-  auto load_values = [&](int s, const Place& p) { load_rows(slot_lds(s) + A::kSlotK + wv * A::kEight, pa.pg.V, p); };
+  auto load_values = [&](int s, const Place& p) { load_rows(slot_lds(s) + A::kSlotK + wv * (kBring / 8 * A::kEight), pa.pg.V, p); };
   // e4m3: sixteen bytes a lane to a place of the wave's own in LDS, a stage later from there into the ring as bf16
-  // (held in registers until then they made the wave spill others).  Lane l brings piece l / 8 of row l % 8: eight lanes
+  // (held in registers until then they made the wave spill others).  Lane l brings piece l / kBring of row l % kBring: eight lanes
   // then write 128 bytes of the ring that lie together (a row's lanes next to each other: an eight-way bank conflict).
-  constexpr int kLanesPerRow = D / 16;              // lanes that share a row
-  constexpr bool kWhole = 8 * kLanesPerRow == 64;  // (64 channels: half of the lanes)
-  uint32_t a_ks = 0u, a_vs = 0u;                    // scales of row lane % 8 of the wave's eight
+  static_assert(kBring * D == 64 * 16, "");
+  uint32_t a_ks = 0u, a_vs = 0u;                    // scales of the wave's row lane % kBring
   auto issue = [&](int s) {
     const int r_stage = stage_row(s);
     const Place p = find(s, r_stage);
     if (cu) load_counts(s, r_stage);
     __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0): what commit read from there has been read
-    const int off = (lane & 7) * ROWB + (lane >> 3) * 16;
-    if (kWhole || lane < 8 * kLanesPerRow) {
-      load_lds(ring_lds + kRawAt + wv * 8 * D, rsrc_of(pa.pg.K, p.at * ROWB, p.rows * ROWB), off);
-      load_lds(ring_lds + kRawAt + A::kRaw + wv * 8 * D, rsrc_of(pa.pg.V, p.at * ROWB, p.rows * ROWB), off);
-    }
-    a_ks = __builtin_amdgcn_raw_buffer_load_b32(buffer(pa.pg.K_scale, p.at * 4, p.rows * 4), (lane & 7) * 4, 0, 0);   // (behind the rows: 0)
-    a_vs = __builtin_amdgcn_raw_buffer_load_b32(buffer(pa.pg.V_scale, p.at * 4, p.rows * 4), (lane & 7) * 4, 0, 0);
+    const int off = lane % kBring * ROWB + lane / kBring * 16;
+    load_lds(ring_lds + kRawAt + wv * 1024, rsrc_of(pa.pg.K, p.at * ROWB, p.rows * ROWB), off);
+    load_lds(ring_lds + kRawAt + A::kRaw + wv * 1024, rsrc_of(pa.pg.V, p.at * ROWB, p.rows * ROWB), off);
+    a_ks = __builtin_amdgcn_raw_buffer_load_b32(buffer(pa.pg.K_scale, p.at * 4, p.rows * 4), lane % kBring * 4, 0, 0);   // (behind the rows: 0)
+    a_vs = __builtin_amdgcn_raw_buffer_load_b32(buffer(pa.pg.V_scale, p.at * 4, p.rows * 4), lane % kBring * 4, 0, 0);
   };
   auto commit = [&](int s) {
     __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0)
     asm volatile("" ::: "memory");
-    const u32x4 ek = *reinterpret_cast<const u32x4*>(raw_all + wv * 8 * D + (lane * 16) % (8 * D));
-    const u32x4 ev = *reinterpret_cast<const u32x4*>(raw_all + A::kRaw + wv * 8 * D + (lane * 16) % (8 * D));
-    float* aux = aux_all + (s & (A::kDepth - 1)) * A::kAux + wv * 8;
+    const u32x4 ek = *reinterpret_cast<const u32x4*>(raw_all + wv * 1024 + lane * 16);
+    const u32x4 ev = *reinterpret_cast<const u32x4*>(raw_all + A::kRaw + wv * 1024 + lane * 16);
+    float* aux = aux_all + (s & (A::kDepth - 1)) * A::kAux + wv * kBring;
     const float ks = __uint_as_float(a_ks) * c, vs = __uint_as_float(a_vs);
-    if (lane < 8) {
+    if (lane < kBring) {
       aux[A::kStage + lane] = ks;
       aux[2 * A::kStage + lane] = fabsf(vs) < __builtin_inff() ? vs : 0.f;
     }
     if (cu) convert_counts(s);
     unsigned char* slot = slot_at(s);
-    const int r = wv * 8 + (lane & 7), piece = (lane >> 3) * 2;
+    const int r = wv * kBring + lane % kBring, piece = lane / kBring * 2;
     // a row of values whose scale is not finite lies there as a row of NaN with a scale of zero
     const bool lost = !(fabsf(vs) < __builtin_inff());
-    if (lane < 8 * kLanesPerRow) {
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        u32x4 k, v;
+    for (int e = 0; e < 2; ++e) {
+      u32x4 k, v;
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
-          k[w] = e4m3_to_bf16(ek[2 * e + w / 2], w & 1);
-          v[w] = lost ? 0x7fc07fc0u : e4m3_to_bf16(ev[2 * e + w / 2], w & 1);
-        }
-        *reinterpret_cast<u32x4*>(slot + A::place(r, piece + e)) = k;
-        *reinterpret_cast<u32x4*>(slot + A::kSlotK + A::place(r, piece + e)) = v;
+      for (int w = 0; w < 4; ++w) {
+        k[w] = e4m3_to_bf16(ek[2 * e + w / 2], w & 1);
+        v[w] = lost ? 0x7fc07fc0u : e4m3_to_bf16(ev[2 * e + w / 2], w & 1);
       }
+      *reinterpret_cast<u32x4*>(slot + A::place(r, piece + e)) = k;
+      *reinterpret_cast<u32x4*>(slot + A::kSlotK + A::place(r, piece + e)) = v;
     }
   };
   // Between stages: every wave's rows that the next one reads have landed, and it reads none of those that will be
@@ -1181,12 +1185,12 @@ __global__ __launch_bounds__(512, 2) void paged_chunk_kernel(ChunkParams kp, Pag
 
 template <bool E4M3, int D>
 hipError_t launch_chunk(const KParams& kp, const PagedAttend& pa, hipStream_t st) {
-  using A = ChunkGeom<D>;
+  using A = ChunkGeom<E4M3, D>;
   const int q_blocks = (int)(((int64_t)pa.rw.max_n * kp.G + A::kBlockQ - 1) / A::kBlockQ);
   static LdsLimitOnce lim;
   const hipError_t e = lim.ensure(reinterpret_cast<const void*>(&paged_chunk_kernel<E4M3, D>), 160 * 1024);
   if (e != hipSuccess) return e;
-  paged_chunk_kernel<E4M3, D><<<dim3(mapped_blocks(pa.pg.n_units, q_blocks * pa.splits)), dim3(512), E4M3 ? A::kLdsE4m3 : A::kLds, st>>>(ChunkParams{kp.G, kp.causal, kp.scale_log2}, pa, q_blocks);
+  paged_chunk_kernel<E4M3, D><<<dim3(mapped_blocks(pa.pg.n_units, q_blocks * pa.splits)), dim3(A::kWaves * 64), E4M3 ? A::kLdsE4m3 : A::kLds, st>>>(ChunkParams{kp.G, kp.causal, kp.scale_log2}, pa, q_blocks);
   return hipSuccess;
 }
 
@@ -1232,24 +1236,25 @@ static int64_t query_blocks(const KParams& kp, int n_units, int max_n, int64_t b
   return (int64_t)n_units * (((int64_t)max_n * kp.G + block - 1) / block);
 }
 bool paged_fits(const KParams& kp, int n_units, int max_n) {
-  return query_blocks(kp, n_units, max_n, kp.dtype == CASK_F32 ? kCols : ChunkGeom<128>::kBlockQ) <= kMostBlocks;
+  return query_blocks(kp, n_units, max_n, kp.dtype == CASK_F32 ? kCols : 256) <= kMostBlocks;
 }
 
 // Which kernel, and how many workgroups share the rows of a block of queries.  By what a call takes, as measured (us):
-// rounds of the 256 compute units, each `start` + `row` for every row that a workgroup goes through; with splits 4 for
+// rounds of the 256 compute units (a column is 128 / 64 channels, or as the line says), each `start` + `row` for every row that a workgroup goes through; with splits 4 for
 // the launch that adds them and their results' way to memory and back at 4 TB/s.
 //   form                       start   us per 1000 rows, 128 / 64 channels
 //   up to 16 query rows          4       9 / 5      (4 units of 32 768 rows 15 in all; 512 of 2100 52)
 //   up to 32                     4      15.5 / 9    (64 units of 4000 rows, 64 query rows 41; 256 of 1500 55)
 //   the same, fp32               4      32 / 32
-//   256, bf16 / e4m3             6      36 / 45, 23 / 27
+//   256, bf16 / e4m3             6      36 / 45
+//   128 of 64 channels           6      23 / 27   (two of them share a compute unit)
 // The form of 256 query rows is slower per row of the cache and takes eight times as many queries along: 4 units of
 // 30 000 rows with 128 / 192 / 256 query rows each 38 / 47 / 53 by 32, 35 / 37 / 40 by 256; 64 of 500 19 / 34 / 36 and
 // 33 / 38 / 44; 256 of 1500 with 64 / 96 / 128 55 / 78 / 101 and 55 / 56 / 57.
 PagedPlan paged_plan(const KParams& kp, int n_units, int max_n, bool e4m3, int window, int sinks, int max_rows) {
   const int64_t m = (int64_t)max_n * kp.G;
   const bool f32 = kp.dtype == CASK_F32, wide = kp.d == 128;
-  auto cost = [&](int64_t block, int least, double start, double per_row, int* splits) {
+  auto cost = [&](int64_t block, int slots, int least, double start, double per_row, int* splits) {
     const int64_t blocks = query_blocks(kp, n_units, max_n, block);
     int64_t rows = max_rows;
     const int64_t tokens = (block < m ? block : m) / kp.G + 1;
@@ -1257,7 +1262,7 @@ PagedPlan paged_plan(const KParams& kp, int n_units, int max_n, bool e4m3, int w
     double best = 0.0;
     for (int s = 1; s <= kMostSplits && (s == 1 || rows >= (int64_t)s * least); ++s) {
       if (s > 1 && (blocks * s > kMostBlocks || n_units * m > kMostBlocks)) break;
-      double c = (double)((blocks * s + 255) / 256) * (start + per_row * 1e-3 * (double)((rows + s - 1) / s));
+      double c = (double)((blocks * s + slots - 1) / slots) * (start + per_row * 1e-3 * (double)((rows + s - 1) / s));
       if (s > 1) c += 4.0 + (double)n_units * m * s * kp.d * 8.0 / 4.0e6;
       if (s == 1 || c < best) best = c, *splits = s;
     }
@@ -1265,11 +1270,11 @@ PagedPlan paged_plan(const KParams& kp, int n_units, int max_n, bool e4m3, int w
   };
   PagedPlan few{false, 1}, many{true, 1};
   const bool two = m > kCols && (!f32 || !wide);
-  const double c_few = cost(two ? 2 * kCols : kCols, 256, 4.0, f32 ? 32.0 : two ? (wide ? 15.5 : 9.0) : (wide ? 9.0 : 5.0), &few.splits);
+  const double c_few = cost(two ? 2 * kCols : kCols, 256, 256, 4.0, f32 ? 32.0 : two ? (wide ? 15.5 : 9.0) : (wide ? 9.0 : 5.0), &few.splits);
   const bool ask_many = (kp.path_flags & CASK_PATH_PAGED_MANY) != 0, ask_few = (kp.path_flags & CASK_PATH_PAGED_FEW) != 0;
   const bool few_fit = query_blocks(kp, n_units, max_n, kCols) <= kMostBlocks;
   if (f32 || (few_fit && (ask_few || (m <= 2 * kCols && !ask_many)))) return few;
-  const double c_many = cost(ChunkGeom<128>::kBlockQ, 128, 6.0, wide ? (e4m3 ? 45.0 : 36.0) : (e4m3 ? 27.0 : 23.0), &many.splits);
+  const double c_many = cost(wide ? 256 : 128, wide ? 256 : 512, 128, 6.0, wide ? (e4m3 ? 45.0 : 36.0) : (e4m3 ? 27.0 : 23.0), &many.splits);
   return c_many < c_few || ask_many || !few_fit ? many : few;
 }
 
