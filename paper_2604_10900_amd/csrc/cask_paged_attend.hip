@@ -1205,11 +1205,19 @@ hipError_t launch_rows_as(const KParams& kp, const PagedAttend& pa, hipStream_t 
   return hipSuccess;
 }
 
+// Which form of the rows kernel (us, 128 channels, 4 heads a unit, e4m3 unless noted):
+//   two groups of 16 query rows instead of one from 17 query rows on: 5 tokens of 256 bf16 units of 1500 rows 43.9 for 47.0 (64 units,
+//     whose rows the caches hold for the second group: 20.5 for 19.0)
+//   four waves where there are more workgroups than compute units, else eight: 1024 units of 600 rows 38.4 / 49.2, 300 of
+//     2100 46.1 / 51.3, 512 52.8 / 55.8; 256 31.5 / 30.6
+//   non-temporal loads from 64 MB of rows on, which a program's other layers push out of the caches before the next step: 256
+//     units of 2100 rows, six caches in turn, 29.1 for 30.8, 128 bf16 units of 1500 22.9 for 24.8, 512 bf16 units of 2100 86.2
+//     for 96.8 (one cache alone, which stays there: 27.9 for 27.0, 23.0 for 23.2)
 template <typename T, bool E4M3, int D>
 hipError_t launch_rows(const KParams& kp, const PagedAttend& pa, int64_t bytes, hipStream_t st) {
   const int64_t m = (int64_t)pa.rw.max_n * kp.G;
   constexpr bool kTwo = sizeof(T) == 2 || D == 64;  // (fp32, 128 channels: two groups do not fit the registers)
-  const bool two = kTwo && m > kCols, nt = bytes > (256ll << 20);
+  const bool two = kTwo && m > kCols, nt = bytes > (64ll << 20);
   const int64_t groups = (int64_t)pa.pg.n_units * ((m + (two ? 2 : 1) * kCols - 1) / ((two ? 2 : 1) * kCols)) * pa.splits;
   auto go = [&](auto f) { return f(kp, pa, st); };
   if constexpr (kTwo)
@@ -1240,14 +1248,14 @@ bool paged_fits(const KParams& kp, int n_units, int max_n) {
 }
 
 // Which kernel, and how many workgroups share the rows of a block of queries.  By what a call takes, as measured (us):
-// rounds of the 256 compute units (a column is 128 / 64 channels, or as the line says), each `start` + `row` for every row that a workgroup goes through; with splits 4 for
+// rounds of the 256 compute units, each `start` + `row` for every row that a workgroup goes through; with splits 4 for
 // the launch that adds them and their results' way to memory and back at 4 TB/s.
-//   form                       start   us per 1000 rows, 128 / 64 channels
+//   query rows                 start   us per 1000 rows, 128 / 64 channels
 //   up to 16 query rows          4       9 / 5      (4 units of 32 768 rows 15 in all; 512 of 2100 52)
 //   up to 32                     4      15.5 / 9    (64 units of 4000 rows, 64 query rows 41; 256 of 1500 55)
 //   the same, fp32               4      32 / 32
-//   256, bf16 / e4m3             6      36 / 45
-//   128 of 64 channels           6      23 / 27   (two of them share a compute unit)
+//   256, bf16 / e4m3             6      36 / 45 (both 128 channels)
+//   128, bf16 / e4m3             6      23 / 27 (both 64 channels, two workgroups a compute unit)
 // The form of 256 query rows is slower per row of the cache and takes eight times as many queries along: 4 units of
 // 30 000 rows with 128 / 192 / 256 query rows each 38 / 47 / 53 by 32, 35 / 37 / 40 by 256; 64 of 500 19 / 34 / 36 and
 // 33 / 38 / 44; 256 of 1500 with 64 / 96 / 128 55 / 78 / 101 and 55 / 56 / 57.

@@ -186,6 +186,21 @@ def test_one_token(dtype, cache, d, G, page_rows):
         _attend(pages, n, start, first, 1, len(lens), seed=G, **kw)
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("dtype,cache", TYPES)
+@pytest.mark.parametrize("units", [5, 300])
+def test_one_token_of_caches_with_room_for_many_rows(dtype, cache, d, units):
+    """Tables far wider than their units' rows, with nothing behind them: the call is dealt out, and its rows loaded,
+    as for caches of many megabytes, unless it is told how many rows there are."""
+    lens = [1 + 37 * u % 130 for u in range(units)]
+    made = plain.make(dtype, cache, d, 3, units=units, page_rows=16, cap_pages=9, seed=units)
+    table = torch.full((units, 8192), -1, dtype=torch.int32, device="cuda")
+    table[:, :made.table.shape[1]] = made.table
+    pages = cask.Pages(made.params, made.K, made.V, made.K_scale, made.V_scale, table)
+    for kw in (dict(), dict(max_rows=130), dict(window=20, sinks=2)):
+        _attend(pages, [1] * units, [x - 1 for x in lens], list(range(units)), 1, units, seed=2, **kw)
+
+
 FORMS = [0, B.PATH_PAGED_FEW, B.PATH_PAGED_MANY]   # the library's choice, blocks of few query rows, blocks of many
 
 
