@@ -697,10 +697,13 @@ struct ChunkGeom {
 //   logits   S[key][query]     = K . Q^T      (lane: query = lane % 32; keys (i & 3) + 8 (i >> 2) + 4 (lane / 32))
 //   values   O[channel][query] += V^T . P     (P as the lane has it: the product's key order is that of S; V^T by
 //                                              transposing reads of four keys)
-// Softmax: weights relative to a reference that follows the largest logit so far only when that has grown by more
-// than 2^8 (results are quotients of two sums with the same reference; nothing overflows below 2^127): then, and
-// only then, the sums are rescaled.  The three parts work on different rows in one turn of the loop -- the logits of
-// the next 32, the weights of these, the values of those before -- so that matrix and vector pipes are both busy.
+// Softmax: weights relative to a reference 2^8 above the largest weight at the time that it was set, which follows only
+// when a logit passes it (results are quotients of two sums with the same reference): then, and only then, the sums are
+// rescaled.  So no weight is larger than one, as in paged_rows_kernel, and a sum overflows where that of the values'
+// magnitudes does.  (With the largest weight itself as the reference, followed 2^8 later, 300 rows of 2^118 gave
+// infinities; the time is the same.  The other end: the weights of e4m3 rows whose scale is below 2^-118 are denormal.)
+// The three parts work on different rows in one turn of the loop -- the logits of the next 32, the weights of these, the
+// values of those before -- so that matrix and vector pipes are both busy.
 // bf16 weights are rounded once (2^-9 of a weight at the most): two terms as for single tokens would cost as many
 // matrix instructions again where these are the bound.
 // Bound: matrix and vector pipes, which a SIMD's two waves keep busy in turn.  2048 x 7 query rows of 4 units behind 16 384 rows:
@@ -899,11 +902,11 @@ __global__ __launch_bounds__(D * 4, 2) void paged_chunk_kernel(ChunkParams kp, P
       a[m] = x.b;
     }
   };
-  constexpr float kLimit = 8.f;
+  constexpr float kHeadroom = 8.f;
   f32x16 acc[CB], s[2];  // s[t & 1]: logits of tile t
   bf16x8 p[2][2];        // p[t & 1]: weights of tile t
   float ref = 0.f, l = 0.f;
-  float limit = kNegInf;            // how far an exponent may lie above the reference: -inf before the first that is seen
+  float limit = kNegInf;            // exponents above it make the reference follow: zero, -inf before the first that is seen
 #pragma unroll
   for (int cb = 0; cb < CB; ++cb) {
     marks[cb / 2] = 0u;
@@ -1000,9 +1003,9 @@ __global__ __launch_bounds__(D * 4, 2) void paged_chunk_kernel(ChunkParams kp, P
   auto follow = [&](f32x16& x, float mx) {
     const u32x2 both = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false));
     const float top = fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1]));
-    const float d = top > limit ? top : 0.f;
+    const float d = top > limit ? top + kHeadroom : 0.f;
     const float corr = limit == kNegInf ? 1.f : __builtin_amdgcn_exp2f(-d);
-    if (top > limit) limit = kLimit;
+    if (top > limit) limit = 0.f;
     ref += d;
 #pragma unroll
     for (int i = 0; i < 16; ++i) x[i] -= d;
@@ -1112,7 +1115,7 @@ __global__ __launch_bounds__(D * 4, 2) void paged_chunk_kernel(ChunkParams kp, P
             for (int cb = 0; cb < CB; ++cb) clean(v[cb], bits, cb);
           }
         }
-        grown_prev = __any(mx > limit) != 0;  // some query's exponents have outgrown its reference, or are its first:
+        grown_prev = __any(mx > limit) != 0;  // some query's exponents have passed its reference, or are its first:
         if (grown_prev) corr = follow(s[half], mx);  // its sums follow when this tile's values join them
         load_k(a, after, half);
         // (bf16: 552 -> 543 us for 2048 x 7 query rows behind 16 384 rows; e4m3, whose waves convert rows meanwhile, lost)

@@ -1,5 +1,6 @@
 """Operators over a paged cache on the GPU against the plain 64-bit form (tests/paged_plain.py)."""
 import ctypes as C
+import math
 
 import pytest
 import torch
@@ -422,6 +423,33 @@ def test_references_that_have_to_follow():
             out = cask.attend_paged(pages, plain.rows([40], [280]), Q.cuda())
             torch.cuda.synchronize()
             plain.check_attend(out, plain.attend(plain.host(pages), Q, [40], [280], [0], 1), "bf16", False)
+
+
+@pytest.mark.parametrize("form", FORMS[1:])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("cache", ["bf16", "e4m3"])
+def test_large_values_stay_finite(cache, d, form):
+    """Values of about 2^117 under logits that first are zero and then grow to 5.4 (2^7.8): no weight is larger than one, so that
+    the sums of 300 rows stay finite, in one workgroup and in several that share the rows."""
+    pages = plain.make("bf16", cache, d, 2, units=1, page_rows=16, cap_pages=20, seed=4, params_kw=dict(path_flags=form))
+    p, n, past = pages.params, 40, 280
+    g = torch.Generator().manual_seed(6)
+    K, V = torch.zeros(1, 320, d), 2.0 ** 117 * (1 + torch.rand(1, 320, d, generator=g))
+    K[0, 64:, 0] = 5.4 / 8.0 * math.sqrt(d)
+    K[0, :64, 1] = torch.randn(64, generator=g)
+    cask.cache_write(pages, plain.rows([320]), K.to(torch.bfloat16).cuda(), V.to(torch.bfloat16).cuda())
+    Q = 0.1 * torch.randn(n, 2, d, generator=g)
+    Q[..., 0] = 8.0
+    Q = Q.to(torch.bfloat16)
+    r = plain.rows([n], [past], [0])
+    want = plain.attend(plain.host(pages), Q, [n], [past], [0], 1)
+    plain.check_attend(cask.attend_paged(pages, r, Q.cuda()), want, "bf16", False)
+    lib, cp, cr, Qd = cask.load(), p.c(), r.c(n), Q.cuda()
+    out = torch.zeros_like(Qd)
+    assert lib.cask_attend_paged(C.byref(cp), C.byref(pages._c), C.byref(cr), Qd.data_ptr(), None, 0, 0, 0, 0, out.data_ptr(), None, 0,
+                                 torch.cuda.current_stream().cuda_stream) == 0
+    torch.cuda.synchronize()
+    plain.check_attend(out, want, "bf16", False)
 
 
 # ---------------------------------------------------------------- together
