@@ -454,7 +454,7 @@ def _current_device() -> int:
 
 class Pages:
     """A paged cache (cask_pages): the pools and who owns which page.  Keep it as long as the cache; what the tensors
-    hold may change at any time.
+    hold may change at any time, p's dtype and head_dim may not (calls refuse that).
 
     K, V      [n_pages, page_rows, d] float32 or bfloat16 (as p.dtype) or float8_e4m3fn; rows one behind the other,
               pages at any common stride of whole rows (both pools may be views of one [n_pages, 2, page_rows, d])
@@ -482,6 +482,7 @@ class Pages:
             assert t is None or (t.is_cuda and t.device == K.device), "device-resident tensors expected"
         self.params, self.K, self.V, self.K_scale, self.V_scale, self.table = p, K, V, K_scale, V_scale, table
         self.device, self._index = K.device, K.device.index
+        self._made_for = p.dtype, p.head_dim   # (the kernels take both from p as it is at the call)
         self._rows_dtype = torch.float32 if p.dtype == F32 else torch.bfloat16   # of the arrays that calls bring
         self.n_units = n_pages if table is None else table.shape[0]
         ptr = [None if t is None else t.data_ptr() for t in (table, K, V, K_scale, V_scale)]
@@ -523,9 +524,10 @@ class Rows:
 def _paged_arrays(pages: Pages, rows: Rows, per_row: int, x: torch.Tensor, y: torch.Tensor) -> int:
     """Rows of a call's two arrays, `per_row` elements each, after the checks that all paged calls share.  Everything lies
     on the current device: the stream a call goes to is that device's."""
-    want, dev, n = pages._rows_dtype, pages.device, x.numel()
+    want, dev, n, p = pages._rows_dtype, pages.device, x.numel(), pages.params
+    assert (p.dtype, p.head_dim) == pages._made_for, "parameters were changed after the cache was made"
     assert x.dtype == want and y.dtype == want, (x.dtype, y.dtype, want)
-    assert x.shape == y.shape and x.shape[-1] == pages.params.head_dim and n % per_row == 0, (x.shape, y.shape)
+    assert x.shape == y.shape and x.shape[-1] == p.head_dim and n % per_row == 0, (x.shape, y.shape)
     assert x.is_contiguous() and y.is_contiguous()
     assert rows.n.numel() == pages.n_units, (rows.n.numel(), pages.n_units)
     assert x.device == dev and y.device == dev and rows.device == dev, (x.device, y.device, rows.device, dev)

@@ -134,6 +134,32 @@ def test_binding_refuses_what_does_not_fit():
         cask.Rows(n, 1)
 
 
+class _OnDevice(torch.Tensor):
+    """A host tensor that says it is on the device: for checks that come before any call of the library."""
+    is_cuda = True
+
+
+@pytest.mark.parametrize("change", [dict(head_dim=128), dict(dtype=B.F32)], ids=str)
+def test_parameters_changed_after_the_cache_was_made(monkeypatch, change):
+    """A cache of other rows than the parameters speak of by now: refused before a kernel takes its pools for larger ones."""
+    on = lambda t: t.as_subclass(_OnDevice)  # noqa: E731
+    monkeypatch.setattr(B, "_current_device", lambda: None)
+    p = cask.Params(dtype=B.BF16, head_dim=64, q_per_kv=1, window=1, budget=2)
+    pool = on(torch.zeros(4, 16, 64).to(torch.float8_e4m3fn))
+    scale = on(torch.ones(4, 16))
+    pages = cask.Pages(p, pool, pool, scale, scale)
+    rows = cask.Rows(on(torch.zeros(4, dtype=torch.int32)), 3)
+    for k, v in change.items():
+        setattr(p, k, v)
+    dt = torch.float32 if p.dtype == B.F32 else torch.bfloat16
+    for dtype in {dt, torch.bfloat16}:
+        x = on(torch.zeros(12, p.head_dim, dtype=dtype))
+        for call in (lambda: cask.cache_write(pages, rows, x, x), lambda: cask.cache_read(pages, rows, x, x),
+                     lambda: cask.attend_paged(pages, rows, x[:, None], out=x[:, None])):
+            with pytest.raises(AssertionError):
+                call()
+
+
 # ---------------------------------------------------------------- the plain form itself
 
 def _host_cache(**kw):
