@@ -331,7 +331,7 @@ size_t cask_attend_workspace_bytes(const cask_params* params, int32_t n_units, i
 typedef struct {
   int32_t type;        /* CASK_E4M3, or params->dtype */
   int32_t n_units;
-  int32_t n_pages;     /* pages of the pools (without a table >= n_units) */
+  int32_t n_pages;     /* pages of the pools (without a table >= n_units); n_pages * page_pitch <= 2^53 */
   int32_t page_rows;   /* a power of two, 16 to 2^20; without a table 1 to 2^29 (CASK_E4M3: a multiple of 16) */
   int64_t page_pitch;  /* pool rows from the start of a page to that of the next, >= page_rows; a row has d
                           elements in K and V, one in the scales */
@@ -350,7 +350,7 @@ typedef struct {
 typedef struct {
   int32_t max_n;        /* HOST: n[u] is taken as at most this; sizes the launch.  max_n * G <= 2^29, n_units * max_n < 2^31 */
   int64_t pitch;        /* >= 1 */
-  int64_t total;        /* rows of the call's arrays: rows outside [0, total) are neither read nor written */
+  int64_t total;        /* rows of the call's arrays: rows outside [0, total) are neither read nor written; <= 2^33 */
   const int32_t* n;     /* DEVICE [n_units]; a negative one counts as 0 */
   const int32_t* start; /* DEVICE [n_units] or NULL: 0.  -2^30 to 2^30 */
   const int64_t* first; /* DEVICE [n_units] or NULL: u * max_n */

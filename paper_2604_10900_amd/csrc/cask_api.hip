@@ -272,12 +272,16 @@ static bool misaligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p)
 // Rows of a unit, and query rows of one: with places held to +-2^30 (a start further out has its rows outside every
 // capacity) and windows to 2^30, no sum or difference of these leaves 32 bits.
 constexpr int kMostUnitRows = 1 << 29;
+// Rows of a call's arrays (a row has 128 bytes at the least) and of a pool (512 at the most): no place's product, below
+// 2^29 * 2^33 rows in array_row and 2^53 rows * 2^9 bytes behind pool_row, leaves 64 bits.
+constexpr int64_t kMostArrayRows = 1ll << 33, kMostPoolRows = 1ll << 53;
 
 // `pointers`: the device pointers are checked as well (not where only sizes are asked for).
 static int resolve_pages(const KParams& kp, const cask_pages* p, PagesView* pg, bool pointers) {
   if (!p || p->n_units < 0) return CASK_EINVAL;
   if (p->type != CASK_E4M3 && p->type != kp.dtype) return CASK_EINVAL;
   if (p->n_pages < 0 || p->page_rows < 1 || p->page_pitch < p->page_rows || p->page_pitch > (1ll << 40)) return CASK_EINVAL;
+  if (p->n_pages > kMostPoolRows / p->page_pitch) return CASK_EINVAL;
   pg->n_units = p->n_units;
   pg->n_pages = p->n_pages;
   pg->table_pitch = p->table_pitch;
@@ -309,7 +313,7 @@ static int resolve_pages(const KParams& kp, const cask_pages* p, PagesView* pg, 
 }
 
 static int resolve_rows(const KParams& kp, const PagesView& pg, const cask_rows* r, RowsView* rw, bool pointers) {
-  if (!r || r->max_n < 0 || r->pitch < 1 || r->total < 0 || r->total > (1ll << 40)) return CASK_EINVAL;
+  if (!r || r->max_n < 0 || r->pitch < 1 || r->total < 0 || r->total > kMostArrayRows) return CASK_EINVAL;
   if ((int64_t)r->max_n * kp.G > kMostUnitRows || (int64_t)r->max_n * pg.n_units > 0x7fffffffll) return CASK_EINVAL;
   if (pointers && pg.n_units > 0 && r->max_n > 0 && !r->n) return CASK_EINVAL;
   rw->max_n = r->max_n;

@@ -391,13 +391,13 @@ __device__ inline int rows_of_unit(const RowsView& rw, int u) {
 __device__ inline int64_t first_of_unit(const RowsView& rw, int u) {
   return rw.first ? rw.first[u] : (int64_t)u * rw.max_n;
 }
-// Place of row t of the call in its arrays, -1 if that is outside them (no product or sum here wraps: 0 <= t < 2^29,
-// and a row this far on is compared before it is multiplied).
+// Place of row t of the call in its arrays, -1 if that is outside them.  Nothing here wraps: 0 <= t < 2^29, and a pitch
+// that is multiplied is less than total <= 2^33.
 __device__ inline int64_t array_row(const RowsView& rw, int64_t first, int t) {
   if (first < 0 || first >= rw.total) return -1;
   const int64_t left = rw.total - 1 - first;
   if (rw.pitch > left && t > 0) return -1;
-  const int64_t at = (int64_t)t * rw.pitch;  // pitch <= total < 2^40 here
+  const int64_t at = (int64_t)t * rw.pitch;
   return at <= left ? first + at : -1;
 }
 // Pool row of row r of unit u, 0 <= r < cap; -1 where no page is.

@@ -64,6 +64,24 @@ def test_rows_that_are_refused(lib, bad):
     assert _calls(lib, rows=_rows(**bad)) == (B.EINVAL,) * 3
 
 
+def test_places_that_would_leave_64_bits_are_refused(lib):
+    """Rows of the arrays: t * pitch with t < 2^29 and pitch < total; places in the pools: entry * page_pitch rows of up to
+    512 bytes.  The largest that fit are taken (as the size that is asked for shows)."""
+    def need(**kw):
+        p = cask.Params(q_per_kv=4, window=1, budget=2).c()
+        pg, rw = dict(n_units=1, table_pitch=1 << 12), dict(max_n=1)
+        for k, v in kw.items():
+            (rw if k == "total" else pg)[k] = v
+        return lib.cask_attend_paged_workspace_bytes(C.byref(p), C.byref(_pages(**pg)), C.byref(_rows(**rw)), 0, 0, 0)
+    assert need(total=1 << 33) > 0
+    assert need(total=(1 << 33) + 1) == 0 and _calls(lib, rows=_rows(total=(1 << 33) + 1)) == (B.EINVAL,) * 3
+    most = (1 << 31) - 1   # pages
+    for fits, too_many in ((dict(n_pages=1 << 13, page_pitch=1 << 40), dict(n_pages=(1 << 13) + 1, page_pitch=1 << 40)),
+                           (dict(n_pages=most, page_pitch=1 << 22), dict(n_pages=most, page_pitch=(1 << 22) + 2))):
+        assert need(**fits) > 0, fits
+        assert need(**too_many) == 0 and _calls(lib, pages=_pages(**too_many)) == (B.EINVAL,) * 3, too_many
+
+
 def test_arguments_that_are_refused(lib):
     assert _calls(lib, K=None) == (B.EINVAL,) * 3 and _calls(lib, V=None) == (B.EINVAL,) * 3
     assert _calls(lib, K=FAKE + 8) == (B.EINVAL,) * 3 and _calls(lib, V=FAKE + 2) == (B.EINVAL,) * 3
