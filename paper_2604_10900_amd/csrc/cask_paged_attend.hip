@@ -790,22 +790,37 @@ __global__ __launch_bounds__(D * 4, 2) void paged_chunk_kernel(ChunkParams kp, P
   };
   // (places in LDS as numbers: a generic pointer is tested for null at every use)
   const int ring_lds = __builtin_amdgcn_readfirstlane((int)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)ring);
+  // Waits and barriers for the written-out loads: to the compiler they touch no memory, and it may move reads and writes of
+  // LDS over them unless it is told.
+  auto wait_for = [](auto what) {
+    asm volatile("" ::: "memory");
+    what();
+    asm volatile("" ::: "memory");
+  };
+  // Loads to LDS, written out: m0 holds the place (reserved: the compiler keeps nothing there, and nothing else here uses it);
+  // between a vector instruction that writes a word of the descriptor and the load that reads it there have to be five wait
+  // states, which the compiler does not see to here: the move's and s_nop's four.
   // A kilobyte to LDS, sixteen bytes a lane.  (Written out because the compiler lets every transposing read wait for
   // all such loads that it knows of: as measured when this was written, a chunk of 2048 x 7 query rows behind 16 384 rows took
   // 695 us so and 559 without that wait.  The waits are in `meet`; the loads return no register.)
   auto load_lds = [&](int dst, u32x4 rs, int off) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(__builtin_amdgcn_readfirstlane(dst)), "v"(off), "s"(rs) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(__builtin_amdgcn_readfirstlane(dst)), "v"(off), "s"(rs) : "memory");
   };
   // bf16: straight to LDS, a KB an instruction.  Lane -> group of four rows, piece, row of the group as they lie there.
   constexpr int kLoads = kBring * A::kRowB / 1024, kGroupLanes = D / 2;   // instructions of a wave's rows; lanes of a group
   auto load_rows = [&](int dst, const unsigned char* pool, const Place& p) {
-    const u32x4 rs = rsrc_of(pool, p.at * ROWB, p.rows * ROWB);
+    static_assert(kLoads == 2, "");
+    int to[2], off[2];
 #pragma unroll
-    for (int j = 0; j < kLoads; ++j) {
+    for (int j = 0; j < 2; ++j) {
       const int grp = j * (64 / kGroupLanes) + lane / kGroupLanes;
       const int piece = (lane % kGroupLanes) / 4 ^ (grp & 1);
-      load_lds(dst + j * 1024 / (8 * A::kRowB) * A::kEight + j * 1024 % (8 * A::kRowB), rs, (grp * 4 + lane % 4) * ROWB + piece * 16);
+      to[j] = __builtin_amdgcn_readfirstlane(dst + j * 1024 / (8 * A::kRowB) * A::kEight + j * 1024 % (8 * A::kRowB));
+      off[j] = (grp * 4 + lane % 4) * ROWB + piece * 16;
     }
+    // (both in one, so that the wait states are taken once)
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dwordx4 %2, %4, 0 offen lds\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %3, %4, 0 offen lds"
+                 ::"s"(to[0]), "s"(to[1]), "v"(off[0]), "v"(off[1]), "s"(rsrc_of(pool, p.at * ROWB, p.rows * ROWB)) : "memory");
   };
   auto slot_at = [&](int s) { return ring + (s & (A::kDepth - 1)) * A::kSlot; };
   auto slot_lds = [&](int s) { return ring_lds + (s & (A::kDepth - 1)) * A::kSlot; };
@@ -813,7 +828,7 @@ __global__ __launch_bounds__(D * 4, 2) void paged_chunk_kernel(ChunkParams kp, P
   auto load_counts = [&](int s, int r_stage) {  // of a stage's rows, by one of the waves
     if (s >= n_stages || r_stage >= pa.count_pitch || wv != (s & (A::kWaves - 1))) return;
     const u32x4 rs = rsrc_of(cu, (int64_t)r_stage * 4, min(pa.count_pitch - r_stage, A::kStage) * 4);  // (behind them: 0, which counts as one)
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(__builtin_amdgcn_readfirstlane(ring_lds + kAuxAt + (s & (A::kDepth - 1)) * A::kAux * 4)),
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(__builtin_amdgcn_readfirstlane(ring_lds + kAuxAt + (s & (A::kDepth - 1)) * A::kAux * 4)),
                  "v"(lane * 4), "s"(rs) : "memory");
   };
   // Counts of stage s into their logarithms, a stage before it: by the wave that asked for them, once they are there (bf16:
@@ -838,7 +853,7 @@ __global__ __launch_bounds__(D * 4, 2) void paged_chunk_kernel(ChunkParams kp, P
     const int r_stage = stage_row(s);
     const Place p = find(s, r_stage);
     if (cu) load_counts(s, r_stage);
-    __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0): what commit read from there has been read
+    wait_for([] { __builtin_amdgcn_s_waitcnt(0xc07f); });  // lgkmcnt(0): what commit read from there has been read
     const int off = lane % kBring * ROWB + lane / kBring * 16;
     load_lds(ring_lds + kRawAt + wv * 1024, rsrc_of(pa.pg.K, p.at * ROWB, p.rows * ROWB), off);
     load_lds(ring_lds + kRawAt + A::kRaw + wv * 1024, rsrc_of(pa.pg.V, p.at * ROWB, p.rows * ROWB), off);
@@ -846,8 +861,7 @@ __global__ __launch_bounds__(D * 4, 2) void paged_chunk_kernel(ChunkParams kp, P
     a_vs = __builtin_amdgcn_raw_buffer_load_b32(buffer(pa.pg.V_scale, p.at * 4, p.rows * 4), lane % kBring * 4, 0, 0);
   };
   auto commit = [&](int s) {
-    __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0)
-    asm volatile("" ::: "memory");
+    wait_for([] { __builtin_amdgcn_s_waitcnt(0x0f70); });  // vmcnt(0)
     const u32x4 ek = *reinterpret_cast<const u32x4*>(raw_all + wv * 1024 + lane * 16);
     const u32x4 ev = *reinterpret_cast<const u32x4*>(raw_all + A::kRaw + wv * 1024 + lane * 16);
     float* aux = aux_all + (s & (A::kDepth - 1)) * A::kAux + wv * kBring;
@@ -876,8 +890,10 @@ __global__ __launch_bounds__(D * 4, 2) void paged_chunk_kernel(ChunkParams kp, P
   // Between stages: every wave's rows that the next one reads have landed, and it reads none of those that will be
   // written over.  bf16: the loads of the stage that ends here may still be under way.
   auto meet = [&]() {
-    __builtin_amdgcn_s_waitcnt(E4M3 ? 0xc07f : 0x0070 | 2 * kLoads);  // lgkmcnt(0), and vmcnt(2 kLoads)
-    __builtin_amdgcn_s_barrier();
+    wait_for([] {
+      __builtin_amdgcn_s_waitcnt(E4M3 ? 0xc07f : 0x0070 | 2 * kLoads);  // lgkmcnt(0), and vmcnt(2 kLoads)
+      __builtin_amdgcn_s_barrier();
+    });
   };
 
   // ---- operands of 32 rows: tile t, half t & 1 of stage t / 2
@@ -1137,7 +1153,7 @@ __global__ __launch_bounds__(D * 4, 2) void paged_chunk_kernel(ChunkParams kp, P
         r_prev = r;
       }
     }
-    __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): the requests of stages behind the last
+    wait_for([] { __builtin_amdgcn_s_waitcnt(0x0f70); });  // vmcnt(0): the requests of stages behind the last
     if (grown_prev) rescale(corr);
 #pragma unroll
     for (int cb = 0; cb < CB; ++cb) {

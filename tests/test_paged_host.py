@@ -178,6 +178,29 @@ def test_parameters_changed_after_the_cache_was_made(monkeypatch, change):
                 call()
 
 
+def test_written_out_loads_wait_for_their_descriptor():
+    """Between a vector instruction that writes a scalar register and a vector memory instruction that reads it lie five wait
+    states; in front of a load in inline assembly the assembly itself has to give them (the compiler may put the
+    descriptor there at the last moment, as when it brings spilled words back).  m0 needs one before a load to LDS."""
+    import os
+    import re
+    from paper_2604_10900_amd import build
+    found = 0
+    for name in build.SOURCES:
+        text = open(os.path.join(build.CSRC, name)).read()
+        for asm in re.findall(r'asm volatile\(\s*"((?:[^"\\]|\\.)*buffer_load(?:[^"\\]|\\.)*)"', text):
+            lines = [ln.split() for ln in asm.replace("\\t", "").split("\\n")]
+            states, since_m0 = 0, None
+            for i, ln in enumerate(lines):
+                if ln[0].startswith("buffer_load"):
+                    assert states >= 5 and (ln[-1] != "lds" or since_m0 >= 1), (name, asm)
+                    found += 1
+                n = int(ln[1], 0) + 1 if ln[0] == "s_nop" else 1
+                states += n
+                since_m0 = 0 if ln[:2] == ["s_mov_b32", "m0,"] else None if since_m0 is None else since_m0 + n
+    assert found >= 4
+
+
 # ---------------------------------------------------------------- the plain form itself
 
 def _host_cache(**kw):
