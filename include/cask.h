@@ -126,7 +126,7 @@ enum {
   CASK_PATH_FORCE_FUSED_SWEEPS = 32, /* W*G <= 512: one scoring launch whatever the number of units */
   CASK_PATH_NARROW_ROWS = 64, /* both scoring sweeps: 64 resident rows per wave (256 per workgroup) whatever the shape */
   CASK_PATH_WIDE_ROWS = 128,  /* both scoring sweeps: 128 resident rows per wave (512 per workgroup) whatever the shape */
-  CASK_PATH_PAGED_FEW = 256,  /* cask_attend_paged: blocks of 16 or 32 query rows whatever the shape */
+  CASK_PATH_PAGED_FEW = 256,  /* cask_attend_paged: blocks of 16 or 32 query rows whatever the shape (up to 2^22 blocks of 16) */
   CASK_PATH_PAGED_MANY = 512  /* cask_attend_paged, bf16: blocks of 256 query rows (64 channels: 128) whatever the shape */
 };
 
@@ -320,14 +320,16 @@ size_t cask_attend_workspace_bytes(const cask_params* params, int32_t n_units, i
  * cask_compress_step's K_out, V_out.  An entry outside [0, n_pages) says that no page is there (not written
  * yet, or given back behind a sliding window): its rows are not written, read as zeros, and no query sees
  * them.  Neither does any call touch rows outside the unit's capacity, table_pitch * page_rows (page_rows
- * without a table) rows.  Pages may be shared by units that only read them; a call that writes one row of a
- * pool for two units leaves either's there.
+ * without a table) rows.  Pages may be shared by units that only read them; what a call leaves in a row of a
+ * pool that it writes for two units is undefined unless both write the same (a row is stored in pieces, its scale
+ * apart).
  *
  * CASK_E4M3 pools hold a row x as 8-bit values q with a float of its own, in the 2 d + 8 bytes that a row of K
  * and V then takes (4 d in bfloat16):
  *     a = max |x_c| over the finite channels, at least 448 * 2^-126,
  *     scale = a / 448,  q_c = 448 x_c / a to the next e4m3 value (ties to even),  x_c ~ q_c * scale;
- * an infinite channel becomes +-448 (the row's largest finite magnitude), a NaN stays one. */
+ * the quotient is taken in float32 (within 2^-22 of itself; ties of bfloat16 rows are exact).  An infinite channel
+ * becomes +-448 (the row's largest finite magnitude), a NaN stays one. */
 typedef struct {
   int32_t type;        /* CASK_E4M3, or params->dtype */
   int32_t n_units;
@@ -361,8 +363,9 @@ typedef struct {
 int cask_cache_write(const cask_params* params, const cask_pages* pages, const cask_rows* rows, const void* K,
                      const void* V, void* hip_stream);
 
-/* Reads rows back into K, V [total, d] (DEVICE, params->dtype, 16-byte aligned): the values a row stands for, rounded
- * once (copies where the pool has the same type); zeros where no page is.  Other rows of K, V are left as they are. */
+/* Reads rows back into K, V [total, d] (DEVICE, params->dtype, 16-byte aligned): the values a row stands for, q_c * scale
+ * in float32, from there rounded to the arrays' type (copies where the pool has the same type); zeros where no page is.
+ * Other rows of K, V are left as they are. */
 int cask_cache_read(const cask_params* params, const cask_pages* pages, const cask_rows* rows, void* K, void* V,
                     void* hip_stream);
 
@@ -372,14 +375,18 @@ int cask_cache_read(const cask_params* params, const cask_pages* pages, const ca
  *     0 <= j < start[u] + n[u];  j <= i where params->causal;  where window > 0, j > i - window or j < sinks;
  * and computes out = sum_j p_j v_j, p = softmax_j(scale * <q, k_j> + ln(count_j)), zeros if it sees none; what rows
  * that it does not see hold, NaN included, has no effect on it (a value that it sees and that is not finite makes
- * its channel of the result not finite).  fp32 accumulation, rounded once.
+ * its channel of the result not finite).  Sums in float32, which stay finite where the sum of the |v_j| that a query sees
+ * does; the result is rounded once.  In bfloat16 the weights p_j are rounded too before they meet the values: in blocks of
+ * few query rows to two bfloat16 terms (2^-16 of a weight), in blocks of many to one (2^-8).  Which of both a call takes
+ * follows from its shape (units, max_n, G, d, types, window, max_rows), so a sequence's rounding depends on the batch
+ * that it is in; params->path_flags with CASK_PATH_PAGED_FEW asks for the first.
  *   count [n_units, count_pitch] DEVICE or NULL, as in cask_attend: the tokens a row stands for (< 1 and rows at or
  *         behind count_pitch: 1)
  *   window, sinks  >= 0; window 0: every row; sinks are used with a window only
  *   (n_units * max_n * G up to 2^26 in float32, 2^30 in bfloat16: CASK_EINVAL where that takes more than 2^22 blocks of
  *   16, of 256 query rows)
- *   max_rows  HOST: about the largest start + n of the units, 0 = the capacity; only a choice of how the work is
- *         dealt out goes by it (the same value gives the same bits)
+ *   max_rows  HOST: about the largest start + n of the units, 0 = the capacity; the choice of kernel and how the work is
+ *         dealt out go by it, never which rows are seen (the same value gives the same bits)
  *   ws    DEVICE, 16-byte aligned: where few queries see many rows, several workgroups share them and leave partial
  *         results there; NULL or fewer bytes than cask_attend_paged_workspace_bytes(): one workgroup does it all. */
 int cask_attend_paged(const cask_params* params, const cask_pages* pages, const cask_rows* rows, const void* Q,

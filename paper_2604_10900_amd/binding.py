@@ -557,7 +557,9 @@ def cache_read(pages: Pages, rows: Rows, K: torch.Tensor, V: torch.Tensor):
 def attend_paged(pages: Pages, rows: Rows, Q: torch.Tensor, count: Optional[torch.Tensor] = None, window: int = 0,
                  sinks: int = 0, max_rows: int = 0, out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Attention of the tokens of `rows` over their units' pages (cask_attend_paged): Q [..., G, d], count [n_units,
-    pitch] int32 or None.  Rows of `out` that no token of the call has are left as they are (zeros if it is made here)."""
+    pitch] int32 or None.  Rows of `out` that no token of the call has are left as they are (zeros if it is made here).
+    bfloat16: the softmax weights are rounded to 2^-16 or, where the shape of the call makes that the faster way, to 2^-8 of
+    themselves; PATH_PAGED_FEW in p.path_flags asks for the first."""
     p = pages.params
     if out is None:
         out = torch.zeros_like(Q)
