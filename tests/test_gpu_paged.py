@@ -452,6 +452,61 @@ def test_large_values_stay_finite(cache, d, form):
     plain.check_attend(out, want, "bf16", False)
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("cache", ["bf16", "e4m3"])
+@pytest.mark.parametrize("G,n", [(4, 2), (7, 3), (4, 8), (1, 33), (4, 40)])
+def test_short_chunks_keep_two_terms(cache, d, G, n):
+    """Several tokens in blocks of few query rows: the weights are two bf16 terms there as for one token (2^-16), also where
+    several workgroups share the rows."""
+    form = 0 if n * G <= 32 else B.PATH_PAGED_FEW
+    for units, past in ((3, [77, 0, 300]), (1, [4000])):
+        pages = plain.make("bf16", cache, d, G, units=units, page_rows=16, cap_pages=-(-(max(past) + n) // 16), seed=n + d, params_kw=dict(path_flags=form))
+        first = [u * n for u in range(units)]
+        for kw in (dict(), dict(window=50, sinks=5)):
+            _attend(pages, [n] * units, past, first, 1, units * n, one=True, **kw)
+
+
+@pytest.mark.parametrize("form", FORMS[1:])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("cache", ["bf16", "e4m3"])
+@pytest.mark.parametrize("rows", [320, 4096])
+def test_references_that_follow_in_every_kernel(cache, d, form, rows):
+    """Logits that grow, or fall, by hundreds along the cache, for each type of rows and each width, also where several
+    workgroups share the rows (4096 of them at least) and their references lie far apart; a page that is missing and counts."""
+    n, past = 40, rows - 40
+    for sign in (1.0, -1.0):
+        pages = plain.make("bf16", cache, d, 2, units=1, page_rows=16, cap_pages=rows // 16, seed=3, params_kw=dict(path_flags=form))
+        g = torch.Generator().manual_seed(8)
+        K, V = torch.randn(1, rows, d, generator=g), torch.randn(1, rows, d, generator=g)
+        K[0, :, 0] = sign * torch.linspace(-40, 40, rows)
+        cask.cache_write(pages, plain.rows([rows]), K.to(torch.bfloat16).cuda(), V.to(torch.bfloat16).cuda())
+        pages.table[0, 5] = -1
+        Q = torch.randn(n, 2, d, generator=g)
+        Q[..., 0] = 60.0
+        Q = Q.to(torch.bfloat16)
+        count = torch.randint(1, 9, (1, 100), generator=g, dtype=torch.int32)
+        r, cp = plain.rows([n], [past], [0]), pages.params.c()
+        need = cask.load().cask_attend_paged_workspace_bytes(C.byref(cp), C.byref(pages._c), C.byref(r.c(n)), 0, 0, 0)
+        assert rows < 4096 or need > 0
+        out = cask.attend_paged(pages, r, Q.cuda(), count=count.cuda())
+        torch.cuda.synchronize()
+        plain.check_attend(out, plain.attend(plain.host(pages), Q, [n], [past], [0], 1, count=count), "bf16", form == B.PATH_PAGED_FEW)
+
+
+@pytest.mark.parametrize("dtype,cache", TYPES)
+def test_single_tokens_and_a_chunk_in_one_call(dtype, cache):
+    """What a program does that takes new sequences in while others go on: one token for most units, hundreds for two,
+    none for one, in token order; the units of a sequence group share the pages of their first rows."""
+    G, d, units = 4, 128, 12
+    new = [1, 1, 1, 250, 1, 0, 1, 1, 400, 1, 1, 1]
+    past = [300, 17, 64, 64, 511, 30, 0, 128, 200, 1, 99, 640]
+    pages = plain.make(dtype, cache, d, G, units=units, page_rows=32, cap_pages=21, seed=5)
+    pages.table[1:8, :2] = pages.table[0, :2]     # (64 rows that eight units read)
+    first = [sum(new[:u]) for u in range(units)]
+    for kw in (dict(), dict(window=100, sinks=6)):
+        _attend(pages, new, past, first, 1, sum(new), seed=3, **kw)
+
+
 # ---------------------------------------------------------------- together
 
 def test_a_step_replays_from_a_graph():
