@@ -350,7 +350,8 @@ typedef struct {
  * sequences back to back: first = tokens before the sequence * heads + head, pitch = heads; arrays [n_units, max_n,
  * ...]: first NULL, pitch 1. */
 typedef struct {
-  int32_t max_n;        /* HOST: n[u] is taken as at most this; sizes the launch.  max_n * G <= 2^29, n_units * max_n < 2^31 */
+  int32_t max_n;        /* HOST: n[u] is taken as at most this; sizes the launch.  max_n * G <= 2^29, n_units * max_n < 2^31.
+                           cask_attend_paged deals out every unit by it: take single tokens and long chunks in two calls */
   int64_t pitch;        /* >= 1 */
   int64_t total;        /* rows of the call's arrays: rows outside [0, total) are neither read nor written; <= 2^33 */
   const int32_t* n;     /* DEVICE [n_units]; a negative one counts as 0 */

@@ -704,10 +704,10 @@ struct ChunkGeom {
 // infinities; the time is the same.  The other end: the weights of e4m3 rows whose scale is below 2^-118 are denormal.)
 // The three parts work on different rows in one turn of the loop -- the logits of the next 32, the weights of these, the
 // values of those before -- so that matrix and vector pipes are both busy.
-// bf16 weights are rounded once (2^-9 of a weight at the most): two terms as for single tokens would cost as many
+// bf16 weights are rounded once (2^-8 of a weight at the most): two terms as for single tokens would cost as many
 // matrix instructions again where these are the bound.
 // Bound: matrix and vector pipes, which a SIMD's two waves keep busy in turn.  2048 x 7 query rows of 4 units behind 16 384 rows:
-// 520 us, 980 TFLOP/s (a library product of 8192^3: 1253); without the exponentials 3 % less, without either product
+// 523 to 542 us, 978 to 944 TFLOP/s (a library product of 8192^3: 1253); without the exponentials 3 % less, without either product
 // 5 to 13 %: no single part holds it up.
 template <bool E4M3, int D>
 __global__ __launch_bounds__(D * 4, 2) void paged_chunk_kernel(ChunkParams kp, PagedAttend pa, int q_blocks) {
