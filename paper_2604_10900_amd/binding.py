@@ -478,6 +478,7 @@ class Pages:
             assert K_scale is None and V_scale is None
         if table is not None:
             assert table.dtype == torch.int32 and table.dim() == 2 and table.is_contiguous()
+            assert table.shape[1] > 0 or table.shape[0] == 0, "a table without pages has no address, and would be none to the library"
         for t in (K, V, K_scale, V_scale, table):
             assert t is None or (t.is_cuda and t.device == K.device), "device-resident tensors expected"
         self.params, self.K, self.V, self.K_scale, self.V_scale, self.table = p, K, V, K_scale, V_scale, table

@@ -178,6 +178,17 @@ def test_parameters_changed_after_the_cache_was_made(monkeypatch, change):
                 call()
 
 
+def test_a_table_without_pages_is_refused(monkeypatch):
+    """A table of no pages a unit has no address: to the library it would be no table at all, where unit u owns page u."""
+    monkeypatch.setattr(B, "_current_device", lambda: None)
+    on = lambda t: t.as_subclass(_OnDevice)  # noqa: E731
+    pool = on(torch.zeros(4, 16, 128, dtype=torch.bfloat16))
+    p = plain.params("bf16")
+    with pytest.raises(AssertionError):
+        cask.Pages(p, pool, pool, table=on(torch.zeros(3, 0, dtype=torch.int32)))
+    assert cask.Pages(p, pool, pool, table=on(torch.zeros(0, 2, dtype=torch.int32))).n_units == 0   # (no units: nothing to own)
+
+
 def test_written_out_loads_wait_for_their_descriptor():
     """Between a vector instruction that writes a scalar register and a vector memory instruction that reads it lie five wait
     states; in front of a load in inline assembly the assembly itself has to give them (the compiler may put the
