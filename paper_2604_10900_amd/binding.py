@@ -515,6 +515,7 @@ class Rows:
         for t, dt in ((start, torch.int32), (first, torch.int64)):
             assert t is None or (t.dtype == dt and t.shape == n.shape and t.device == n.device and t.is_contiguous())
         self.n, self.start, self.first, self.max_n, self.pitch = n, start, first, int(max_n), int(pitch)
+        assert self.max_n >> 31 in (0, -1) and self.pitch >> 63 in (0, -1), "max_n has 32 bits, pitch 64"
         self.device = n.device
         self._ptr = [None if t is None else t.data_ptr() for t in (n, start, first)]
 
@@ -565,6 +566,7 @@ def attend_paged(pages: Pages, rows: Rows, Q: torch.Tensor, count: Optional[torc
     if out is None:
         out = torch.zeros_like(Q)
     assert Q.shape[-2] == p.q_per_kv
+    assert (window | sinks | max_rows) >> 31 in (0, -1), "window, sinks and max_rows have 32 bits"
     cr = rows.c(_paged_arrays(pages, rows, p.q_per_kv * p.head_dim, Q, out))
     if count is not None:
         assert count.dtype == torch.int32 and count.dim() == 2 and count.shape[0] == pages.n_units and count.is_contiguous()

@@ -189,6 +189,22 @@ def test_a_table_without_pages_is_refused(monkeypatch):
     assert cask.Pages(p, pool, pool, table=on(torch.zeros(0, 2, dtype=torch.int32))).n_units == 0   # (no units: nothing to own)
 
 
+def test_numbers_of_more_than_32_bits_are_refused(monkeypatch):
+    """A window, a number of first rows or of rows that C would take for another one (its lowest 32 bits)."""
+    on = lambda t: t.as_subclass(_OnDevice)  # noqa: E731
+    monkeypatch.setattr(B, "_current_device", lambda: None)
+    pool, n = on(torch.zeros(4, 16, 128, dtype=torch.bfloat16)), on(torch.zeros(4, dtype=torch.int32))
+    pages, q = cask.Pages(plain.params("bf16"), pool, pool), on(torch.zeros(4, 1, 128, dtype=torch.bfloat16))
+    rows = cask.Rows(n, 1)
+    for kw in (dict(window=(1 << 32) + 5), dict(window=7, sinks=1 << 31), dict(max_rows=(1 << 32) + 1)):
+        with pytest.raises(AssertionError):
+            cask.attend_paged(pages, rows, q, out=q, **kw)
+    with pytest.raises(AssertionError):
+        cask.Rows(n, (1 << 32) + 1)
+    with pytest.raises(AssertionError):
+        cask.Rows(n, 1, pitch=(1 << 64) + 1)
+
+
 def test_written_out_loads_wait_for_their_descriptor():
     """Between a vector instruction that writes a scalar register and a vector memory instruction that reads it lie five wait
     states; in front of a load in inline assembly the assembly itself has to give them (the compiler may put the
